@@ -20,7 +20,8 @@
  *    segblocks_block_conv3x3, segblocks_block_conv_ex,
  *    segblocks_block_conv_chain, segblocks_block_conv_down and segblocks_layer
  *    take it as a `workspace` pointer with its size `ws_bytes` (and so do the
- *    two gradients of the convolution).  The size of a call depends only on
+ *    two gradients of the convolution, segblocks_log_probs and
+ *    segblocks_orthogonalize).  The size of a call depends only on
  *    its shapes, capacities and device, and is given by
  *    segblocks_block_conv3x3_workspace_size,
  *    segblocks_block_conv_ex_workspace_size,
@@ -505,6 +506,82 @@ int segblocks_stem_blocks(const void* x, int dtype, int layout, int N, int C_in,
 int segblocks_maxpool_blocks(const void* hi, const void* lo, int dtype, int layout, int N, int C, int H,
                              int W, const uint8_t* mask, int bs, void* hi_out, void* lo_out, int hi_cap,
                              int lo_cap, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * The two ends of a training step around the convolutions: the loss of class
+ * scores with its gradient, and the update of a filter from its gradient.
+ * ------------------------------------------------------------------------ */
+
+/* Log probabilities of class scores.  A row is a pixel of logits [N,C,H,W]
+ * (or one of N tokens with C scores: H = W = 1); its scores z are the first C
+ * of the C_buf >= C channels of the buffer (a convolution writes multiples of
+ * eight, a vocabulary is padded), which holds [N][C_buf][H][W] (SB_NCHW) or
+ * [N][H][W][C_buf] (SB_NHWC).  With lse = ln sum_j exp(z_j) and
+ * p_j = exp(z_j - lse), per row, fp32:
+ *   logp      z_label - lse for labels [N][H][W] (int64); 0 where the label is
+ *             `ignore`, NaN where it is any other value outside [0, C)
+ *   lse
+ *   entropy   -sum_j p_j ln p_j
+ *   top_logp, top_index (int32)  the topk (0 <= topk <= 64, topk <= C) largest
+ *             z in falling order, equal ones by class, lower first:
+ *             [N][topk][H][W] (SB_NCHW) or [N][H][W][topk] (SB_NHWC)
+ * labels and logp are both NULL or both given; entropy may be NULL; top_* are
+ * NULL with topk = 0.  A class at -inf has probability 0 and adds nothing to
+ * the entropy; a row with every class at -inf has lse, logp and top_logp -inf
+ * and entropy 0.  A row that holds NaN or +inf has NaN for lse, logp, entropy
+ * and top_logp (NaN ranks above every number).  At most 2^31 - 1 rows and
+ * classes.  Needs a workspace where few rows are split over several
+ * workgroups: segblocks_log_probs_workspace_size. */
+int segblocks_log_probs(const void* logits, int dtype, int layout, int N, int C, int H, int W, int C_buf,
+                        const int64_t* labels, long long ignore, int topk, float* logp, float* lse, float* entropy,
+                        float* top_logp, int32_t* top_index, void* workspace, size_t ws_bytes, hipStream_t stream);
+int segblocks_log_probs_workspace_size(int dtype, int layout, int N, int C, int H, int W, int C_buf, int topk,
+                                       size_t* bytes);
+
+/* Gradient of segblocks_log_probs with respect to the scores, from the
+ * gradients of its results: with g the row's d_logp (0 where the label is
+ * ignored), g_i its d_top, G = g + sum_i g_i and g_H its d_entropy,
+ *   dlogits_j = [j = label] g + sum_i [j = top_index_i] g_i
+ *               - p_j (G + g_H (ln p_j + entropy)),
+ * in fp32, rounded once.  lse, entropy and top_index are the forward call's;
+ * d_logp (with labels), d_entropy (with entropy) and d_top (with top_index,
+ * topk > 0) may each be NULL, but not all three.  A row with every class at
+ * -inf has the gradient 0; a label or top_index outside [0, C) (and not
+ * `ignore`) makes its row NaN.  dlogits is laid out like logits with C_dbuf
+ * channels, of which the first C are written and the others left as they
+ * are. */
+int segblocks_log_probs_backward(const void* logits, int dtype, int layout, int N, int C, int H, int W, int C_buf,
+                                 const int64_t* labels, long long ignore, const float* lse, const float* d_logp,
+                                 const float* entropy, const float* d_entropy, int topk, const int32_t* top_index,
+                                 const float* d_top, int C_dbuf, void* dlogits, hipStream_t stream);
+
+/* One update of segblocks_orthogonalize: `batch` matrices of rows x cols in
+ * row-major memory (a filter [C_out,C_in,K,K] is C_out rows of C_in*K*K in
+ * either layout), `ld` elements between rows and `batch_stride` between
+ * matrices.  Device pointers. */
+typedef struct {
+    const void* update;
+    void* out;
+    int batch, rows, cols;
+    long long ld, ld_out, batch_stride, batch_stride_out;
+} sb_matrix;
+
+/* Orthogonalises updates by Newton-Schulz products, as the Muon optimiser
+ * does with the momentum of a filter's gradient: for each matrix G of every
+ * entry of `matrices` (HOST array)
+ *   X = G / (|G|_F + eps), then `steps` times
+ *   X <- a X + (b A + c A A) X,  A = X X^T (the products on the shorter side:
+ *   a matrix with more rows than columns is taken transposed),
+ * written to out in `dtype`.  coefficients: HOST array of a, b, c for every
+ * step (3 * steps).  1 <= steps <= 32, eps >= 0; a matrix of zeros gives
+ * zeros, one with NaN or an infinity gives NaN.  The sums are fp32; matrices
+ * between the products are held to 22 bits or more, so the result is that of
+ * an fp32 iteration also for a 16-bit update, rounded once.  Workspace:
+ * segblocks_orthogonalize_workspace_size (a function of the entries' sizes,
+ * pointers not looked at). */
+int segblocks_orthogonalize(const sb_matrix* matrices, int count, int dtype, int steps, const double* coefficients,
+                            double eps, void* workspace, size_t ws_bytes, hipStream_t stream);
+int segblocks_orthogonalize_workspace_size(const sb_matrix* matrices, int count, int dtype, size_t* bytes);
 
 /* Description of the last failure on the calling thread ("" if none).  The
  * string stays valid until the next call on the same thread. */

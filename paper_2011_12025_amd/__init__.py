@@ -12,6 +12,7 @@ convolution that applies the same filters to both block stacks.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import functools
 
@@ -24,7 +25,9 @@ __all__ = ["count", "split", "pad", "conv3x3", "combine", "block_conv3x3", "bloc
            "layer_workspace_size", "policy_heuristic", "combine_backward", "split_backward", "pad_backward",
            "conv3x3_backward_data", "conv3x3_backward_weight", "layer_backward", "pad_halo", "conv_halo",
            "maxpool_halo", "block_conv_chain", "block_conv_chain_workspace_size", "block_conv_chain_reads_half",
-           "block_conv_down", "split_pad", "pad_split_backward", "stem_pool", "stem_blocks", "maxpool_blocks", "stem_fits"]
+           "block_conv_down", "split_pad", "pad_split_backward", "stem_pool", "stem_blocks", "maxpool_blocks", "stem_fits",
+           "log_probs", "log_probs_workspace_size", "log_probs_backward", "orthogonalize",
+           "orthogonalize_workspace_size"]
 
 _DT = {torch.float32: _b.SB_F32, torch.float16: _b.SB_F16, torch.bfloat16: _b.SB_BF16}
 
@@ -653,6 +656,273 @@ def layer_backward(x: torch.Tensor, mask: torch.Tensor, bs: int, weight: torch.T
     dw, db = conv3x3_backward_weight(hp, lp, dho, dlo_o, mask, bs, H, W, bias=bias, layout=layout)
     dhp, dlp = conv3x3_backward_data(dho, dlo_o, mask, bs, H, W, weight, layout=layout)
     return pad_split_backward(dhp, dlp, mask, bs, H, W, layout=layout, sampling=sampling), dw, db
+
+
+# ---------------------------------------------------------------------------
+# The two ends of a training step: the loss of class scores with its gradient,
+# and the update of a filter from its gradient
+# ---------------------------------------------------------------------------
+
+@contextlib.contextmanager
+def _nothing():
+    yield
+
+
+def _on(t: torch.Tensor):
+    """The device of t as the current one for a call that launches there."""
+    index = t.get_device()
+    if index < 0:
+        raise ValueError(f"expected a cuda tensor, but got one on {t.device}")
+    return _nothing() if index == torch.cuda.current_device() else torch.cuda.device(index)
+
+
+def _scores(t: torch.Tensor, what: str = "logits"):
+    """(layout, N, C, H, W, C_buf) of class scores: a map [N, C, H, W] in either
+    memory format or rows [R, C] / [B, S, C], whose classes may be the first C
+    of a wider buffer (a slice of its channels)."""
+    if t.dim() == 4:
+        N, C, H, W = t.shape
+        sn, sc, sh, sw = t.stride()
+        if C == 1 or sc == 1:  # channels last
+            c = sw if W > 1 else sh if H > 1 else sn if N > 1 else C
+            if c >= C and (H == 1 or sh == W * c) and (N == 1 or sn == H * W * c):
+                return _b.SB_NHWC, N, C, H, W, c
+        P = H * W
+        if (W == 1 or sw == 1) and (H == 1 or sh == W) and (C == 1 or sc == P):
+            if N == 1:
+                return _b.SB_NCHW, N, C, H, W, C
+            if sn % P == 0 and sn // P >= C:
+                return _b.SB_NCHW, N, C, H, W, sn // P
+        raise ValueError(f"{what} must be contiguous or channels_last, or the first channels of such a map")
+    if t.dim() == 2 or t.dim() == 3:
+        C = t.shape[-1]
+        rows = t.shape[0] if t.dim() == 2 else t.shape[0] * t.shape[1]
+        lead = [(n, s) for n, s in zip(t.shape[:-1], t.stride()[:-1]) if n > 1]
+        c = lead[-1][1] if lead else C
+        if (C == 1 or t.stride(-1) == 1) and c >= C and (len(lead) < 2 or lead[0][1] == lead[1][0] * c):
+            return _b.SB_NHWC, rows, C, 1, 1, c
+        raise ValueError(f"{what} must be rows of contiguous scores at one distance")
+    raise ValueError(f"{what} must be [rows, classes], [batch, rows, classes] or [N, classes, H, W]")
+
+
+def _sizes(t: torch.Tensor):
+    s = _scores(t)
+    if max(s) >= 1 << 31:
+        raise ValueError("at most 2^31 - 1 rows, classes and channels")
+    return s
+
+
+def _row_shapes(t: torch.Tensor):
+    """Shape of one value a row of scores t, and of k a row (as a function)."""
+    if t.dim() == 4:
+        return (t.shape[0], *t.shape[2:]), lambda k: (t.shape[0], k, *t.shape[2:])
+    return tuple(t.shape[:-1]), lambda k: (*t.shape[:-1], k)
+
+
+def _row_values(v, like: torch.Tensor, shape, dtype: torch.dtype, what: str, layout=None):
+    """v (or None), checked to hold one value a row (or top_* values in the
+    call's memory format), dense."""
+    if v is None:
+        return None
+    if v.dtype != dtype or tuple(v.shape) != tuple(shape):
+        raise ValueError(f"{what} must be a {dtype} tensor of shape {tuple(shape)}, got {v.dtype} {tuple(v.shape)}")
+    if v.device != like.device:
+        raise ValueError(f"{what} is on {v.device}, the scores on {like.device}")
+    return v.contiguous() if layout is None or v.dim() != 4 else v.contiguous(memory_format=_fmt(layout))
+
+
+def log_probs_workspace_size(dtype: torch.dtype, layout: int, N: int, C: int, H: int, W: int, C_buf: int,
+                             topk: int = 0) -> int:
+    """Bytes of workspace that log_probs needs for these shapes (0 = none);
+    rows of tokens are N rows with H = W = 1 in SB_NHWC."""
+    return _query("segblocks_log_probs_workspace_size", _DT[dtype], layout, N, C, H, W, C_buf, topk)
+
+
+def log_probs(logits: torch.Tensor, labels=None, topk: int = 0, entropy: bool = True, ignore: int = -100,
+              workspace=None):
+    """Log probabilities of class scores, for a map [N, C, H, W] (classes are
+    channels) or rows [R, C] / [B, S, C]; the classes may be the first ones of a
+    wider buffer (``scores[:, :19]`` of a 24-channel map).
+
+    Returns (logp, lse, entropy, top_logp, top_index): the log probability of
+    ``labels`` (int64, one a row; 0 where the label is ``ignore``), the
+    log-sum-exp, the entropy, and the ``topk`` (at most 64) likeliest classes with
+    their log probabilities, shaped [N, topk, H, W] (in the scores' memory format)
+    or [..., topk]; float32 and int32, None for what is not asked for.  Equal
+    scores rank by class, lower first.  ``workspace`` as in block_conv3x3, sized
+    by log_probs_workspace_size()."""
+    layout, N, C, H, W, c_buf = _sizes(logits)
+    one, many = _row_shapes(logits)
+    labels = _row_values(labels, logits, one, torch.int64, "labels")
+    dev = logits.device
+
+    def new(dtype=torch.float32):
+        return torch.empty(one, dtype=dtype, device=dev)
+
+    def new_top(dtype):
+        if logits.dim() == 4:
+            return torch.empty(many(topk), dtype=dtype, device=dev, memory_format=_fmt(layout))
+        return torch.empty(many(topk), dtype=dtype, device=dev)
+
+    if topk < 0 or topk > min(64, C):
+        raise ValueError(f"topk must be in [0, min(64, classes)], got {topk}")
+    dt = _dt(logits)
+    with _on(logits):
+        logp, lse, ent = None if labels is None else new(), new(), new() if entropy else None
+        tl, ti = (new_top(torch.float32), new_top(torch.int32)) if topk else (None, None)
+        if logits.numel():
+            need = _need("segblocks_log_probs_workspace_size", dt, layout, N, C, H, W, c_buf, topk)
+            wp, wn, _keep = _ws(need, dev, workspace)
+            _b.call("segblocks_log_probs", _ptr(logits), dt, layout, N, C, H, W, c_buf, _ptr(labels), ignore, topk,
+                    _ptr(logp), _ptr(lse), _ptr(ent), _ptr(tl), _ptr(ti), wp, wn, _stream(logits))
+        elif C == 0:
+            raise ValueError("no classes")
+    return logp, lse, ent, tl, ti
+
+
+def log_probs_backward(logits: torch.Tensor, labels, lse: torch.Tensor, d_logp=None, entropy=None, d_entropy=None,
+                       top_index=None, d_top=None, ignore: int = -100, out=None):
+    """Gradient of log_probs with respect to the scores, in their type: from the
+    gradients of logp, entropy and top_logp (each may be None, not all three;
+    float32, shaped like those results) and the forward call's labels, lse,
+    entropy and top_index.  ``out``: a tensor shaped and ordered like ``logits``
+    to write to, such as the first channels of the map that a layer's backward
+    pass takes (its other channels are left as they are)."""
+    layout, N, C, H, W, c_buf = _sizes(logits)
+    one, many = _row_shapes(logits)
+    labels = _row_values(labels, logits, one, torch.int64, "labels")
+    f32 = torch.float32
+    lse, d_logp, entropy, d_entropy = (_row_values(v, logits, one, f32, n) for v, n in (
+        (lse, "lse"), (d_logp, "d_logp"), (entropy, "entropy"), (d_entropy, "d_entropy")))
+    topk = 0
+    if d_top is not None:
+        if top_index is None:
+            raise ValueError("d_top needs top_index")
+        topk = top_index.shape[1 if logits.dim() == 4 else -1]
+        top_index = _row_values(top_index, logits, many(topk), torch.int32, "top_index", layout)
+        d_top = _row_values(d_top, logits, many(topk), f32, "d_top", layout)
+        if topk == 0:
+            top_index = d_top = None
+    else:
+        top_index = None
+    with _on(logits):
+        if out is None:
+            out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device,
+                              memory_format=_fmt(layout) if logits.dim() == 4 else torch.contiguous_format)
+        if out.dtype != logits.dtype or out.shape != logits.shape or out.device != logits.device:
+            raise ValueError("out must have the scores' type, shape and device")
+        c_out = _buf_channels(out, layout)
+        if logits.numel():
+            _b.call("segblocks_log_probs_backward", _ptr(logits), _dt(logits), layout, N, C, H, W, c_buf, _ptr(labels),
+                    ignore, _ptr(lse), _ptr(d_logp), _ptr(entropy), _ptr(d_entropy), topk, _ptr(top_index), _ptr(d_top),
+                    c_out, _ptr(out), _stream(logits))
+    return out
+
+
+def _buf_channels(t: torch.Tensor, layout: int) -> int:
+    """C_buf of a tensor of scores that has to be in `layout`."""
+    got, N, C, H, W, c = _scores(t, "out")
+    if c >= 1 << 31:
+        raise ValueError("at most 2^31 - 1 channels")
+    if got != layout:
+        # one of the two where both describe the memory: a single pixel, or a single class
+        if not (H * W == 1 or (C == 1 and c == 1)):
+            raise ValueError("out must share the scores' memory format")
+    return c
+
+
+def _matrix(t: torch.Tensor):
+    """(batch, rows, cols, distance of rows, distance of matrices) of an update
+    in row-major memory; a matrix in column-major memory is taken transposed."""
+    if t.dim() == 4:
+        layout_of(t)  # contiguous or channels_last: filters of C_out rows either way
+        n = t.shape[1] * t.shape[2] * t.shape[3]
+        return 1, t.shape[0], n, n, 0
+    if t.dim() not in (2, 3):
+        raise ValueError("an update is a matrix, a batch of matrices or a filter [C_out, C_in, K, K]")
+    m, n = t.shape[-2:]
+    sm, sn = t.stride()[-2:]
+    batch, sb = (t.shape[0], t.stride(0)) if t.dim() == 3 else (1, 0)
+    if batch == 1:
+        sb = 0
+    if (n == 1 or sn == 1) and (m == 1 or sm >= n):
+        return batch, m, n, sm if m > 1 else n, sb
+    if (m == 1 or sm == 1) and (n == 1 or sn >= m):
+        return batch, n, m, sn if n > 1 else m, sb
+    raise ValueError("the rows or the columns of an update must be contiguous")
+
+
+def _matrices(updates, outs=None):
+    mats = (_b.Matrix * len(updates))()
+    for i, t in enumerate(updates):
+        q = mats[i]
+        q.batch, q.rows, q.cols, q.ld, q.batch_stride = _matrix(t)
+        q.update = t.data_ptr()
+        if outs is None:
+            q.ld_out, q.batch_stride_out = q.cols, q.rows * q.cols
+        else:
+            batch, rows, cols, q.ld_out, q.batch_stride_out = _matrix(outs[i])
+            if (batch, rows, cols) != (q.batch, q.rows, q.cols):
+                raise ValueError(f"out {i} must have its update's order of rows and columns")
+            q.out = outs[i].data_ptr()
+    return mats
+
+
+def orthogonalize_workspace_size(updates) -> int:
+    """Bytes of workspace that orthogonalize needs for these updates (their
+    shapes and type count)."""
+    updates = [updates] if isinstance(updates, torch.Tensor) else list(updates)
+    n = ctypes.c_size_t(0)
+    _b.call("segblocks_orthogonalize_workspace_size", _matrices(updates), len(updates), _dt(updates[0]), ctypes.byref(n))
+    return int(n.value)
+
+
+def orthogonalize(updates, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315), eps: float = 1e-7, out=None,
+                  workspace=None):
+    """Orthogonalised updates by Newton-Schulz products, as the Muon optimiser
+    makes them of a filter's (momentum of the) gradient: X = G / (|G| + eps), then
+    ``steps`` times X <- a X + (b A + c A A) X with A = X X^T, on the shorter side.
+
+    ``updates``: a matrix [m, n], a batch of them [B, m, n] or a filter [C_out,
+    C_in, K, K] (taken as [C_out, C_in K K]), or a list of such tensors of one
+    type and device, which go through the same launches.  ``coefficients``: (a, b,
+    c), or one such triple for every step.  Returns tensors shaped and ordered
+    like the updates (``out`` if given).  ``workspace`` as in block_conv3x3, sized
+    by orthogonalize_workspace_size()."""
+    single = isinstance(updates, torch.Tensor)
+    updates = [updates] if single else list(updates)
+    if not updates:
+        return []
+    ref = updates[0]
+    dt = _dt(ref)
+    for t in updates:
+        if t.dtype != ref.dtype or t.device != ref.device:
+            raise ValueError("the updates of a call share the type and the device")
+    if not 1 <= steps <= 32:
+        raise ValueError(f"steps must be in [1, 32], got {steps}")
+    coef = [float(c) for row in coefficients for c in (row if isinstance(row, (tuple, list)) else (row,))]
+    if len(coef) == 3:
+        coef = coef * steps
+    if len(coef) != 3 * steps:
+        raise ValueError("coefficients must be (a, b, c), or one such triple for every step")
+    with _on(ref):
+        if out is None:
+            outs = [torch.empty_like(t) for t in updates]
+        else:
+            outs = [out] if isinstance(out, torch.Tensor) else list(out)
+            if len(outs) != len(updates) or any(o.shape != t.shape or o.dtype != t.dtype or o.device != t.device or
+                                                (t.dim() == 4 and layout_of(o) != layout_of(t))
+                                                for o, t in zip(outs, updates)):
+                raise ValueError("out must have the updates' shapes, type, device and memory format")
+        some = [(t, o) for t, o in zip(updates, outs) if t.numel()]
+        if some:
+            mats = _matrices(*zip(*some))
+            n = ctypes.c_size_t(0)
+            _b.call("segblocks_orthogonalize_workspace_size", mats, len(some), dt, ctypes.byref(n))
+            wp, wn, _keep = _ws(int(n.value), ref.device, workspace)
+            _b.call("segblocks_orthogonalize", mats, len(some), dt, steps, (ctypes.c_double * len(coef))(*coef),
+                    float(eps), wp, wn, _stream(ref))
+    return outs[0] if single else outs
 
 
 # ---------------------------------------------------------------------------

@@ -30,14 +30,25 @@ EXPORTS = ["segblocks_count", "segblocks_split", "segblocks_pad", "segblocks_pad
            "segblocks_conv3x3_backward_data", "segblocks_conv3x3_backward_data_workspace_size",
            "segblocks_conv3x3_backward_weight", "segblocks_conv3x3_backward_weight_workspace_size",
            "segblocks_pad_halo", "segblocks_conv_halo", "segblocks_maxpool_halo", "segblocks_block_conv_down", "segblocks_split_pad", "segblocks_pad_split_backward", "segblocks_stem_pool",
-           "segblocks_stem_blocks", "segblocks_maxpool_blocks", "segblocks_last_error"]
+           "segblocks_stem_blocks", "segblocks_maxpool_blocks", "segblocks_log_probs",
+           "segblocks_log_probs_workspace_size", "segblocks_log_probs_backward", "segblocks_orthogonalize",
+           "segblocks_orthogonalize_workspace_size", "segblocks_last_error"]
 
 SB_OK, SB_EINVAL, SB_ESHAPE, SB_EHIP, SB_ENOMEM = 0, -1, -2, -3, -4
 
 _P = ctypes.c_void_p
 _I = ctypes.c_int
 _Z = ctypes.c_size_t
+_L = ctypes.c_longlong
 _ZP = ctypes.POINTER(ctypes.c_size_t)
+
+
+class Matrix(ctypes.Structure):
+    """sb_matrix: one update of segblocks_orthogonalize."""
+    _fields_ = [("update", _P), ("out", _P), ("batch", _I), ("rows", _I), ("cols", _I), ("ld", _L), ("ld_out", _L),
+                ("batch_stride", _L), ("batch_stride_out", _L)]
+
+
 _SIGS = {
     "segblocks_count": [_P, _I, _I, _I, ctypes.POINTER(_I), ctypes.POINTER(_I), _P],
     "segblocks_split": [_P, _I, _I, _I, _I, _I, _I, _P, _I, _P, _I, _P, _I, _P],
@@ -81,6 +92,12 @@ _SIGS = {
     "segblocks_stem_pool": [_P, _I, _I, _I, _I, _I, _I, _P, _P, _I, _P, _P],
     "segblocks_stem_blocks": [_P, _I, _I, _I, _I, _I, _I, _P, _I, _P, _P, _I, _I, _P, _I, _P, _I, _P],
     "segblocks_maxpool_blocks": [_P, _P, _I, _I, _I, _I, _I, _I, _P, _I, _P, _P, _I, _I, _P],
+    "segblocks_log_probs": [_P, _I, _I, _I, _I, _I, _I, _I, _P, _L, _I, _P, _P, _P, _P, _P, _P, _Z, _P],
+    "segblocks_log_probs_workspace_size": [_I] * 8 + [_ZP],
+    "segblocks_log_probs_backward": [_P, _I, _I, _I, _I, _I, _I, _I, _P, _L, _P, _P, _P, _P, _I, _P, _P, _I, _P, _P],
+    "segblocks_orthogonalize": [ctypes.POINTER(Matrix), _I, _I, _I, ctypes.POINTER(ctypes.c_double), ctypes.c_double,
+                                _P, _Z, _P],
+    "segblocks_orthogonalize_workspace_size": [ctypes.POINTER(Matrix), _I, _I, _ZP],
     "segblocks_maxpool": [_P, _I, _I, _I, _I, _I, _I, _I, _I, _I, _P, _P],
 }
 

@@ -1058,4 +1058,185 @@ int segblocks_maxpool_blocks(const void* hi, const void* lo, int dtype, int layo
     return hip_status(fn, sb::launch_pool_blocks(dtype, g, mask, hi, lo, hi_out, lo_out, hi_cap, lo_cap, stream));
 }
 
+namespace {
+
+// Checks of both log-probability calls; rows and pixels of a plane go to R, P.
+int check_scores(const char* fn, int dtype, int layout, int N, int C, int H, int W, int C_buf, int topk, long long* R,
+                 long long* P) {
+    if (dtype != SB_F32 && dtype != SB_F16 && dtype != SB_BF16) return fail(SB_EINVAL, fn, "bad dtype %d", dtype);
+    if (layout != SB_NCHW && layout != SB_NHWC) return fail(SB_EINVAL, fn, "bad layout %d", layout);
+    if (N <= 0 || C <= 0 || H <= 0 || W <= 0)
+        return fail(SB_EINVAL, fn, "N, C, H, W must be positive (got %d, %d, %d, %d)", N, C, H, W);
+    if (C_buf < C) return fail(SB_EINVAL, fn, "the buffer's channels must hold the classes (got %d for %d)", C_buf, C);
+    if (topk < 0 || topk > sb::logp_max_top() || topk > C)
+        return fail(SB_EINVAL, fn, "topk must be in [0, min(%d, C)] (got %d)", sb::logp_max_top(), topk);
+    const long long HW = (long long)H * W;  // < 2^62
+    if (HW >= (1LL << 31) || N * HW >= (1LL << 31) || N * HW * C_buf > (1LL << 40))
+        return fail(SB_ESHAPE, fn, "problem too large (%lld rows of %d)", HW >= (1LL << 31) ? HW : N * HW, C_buf);
+    *R = N * HW;
+    *P = layout == SB_NCHW ? HW : 1;
+    return SB_OK;
+}
+
+// Bytes from the first to the last score of the classes.
+long long scores_bytes(long long R, long long P, int C, int C_buf, int es) {
+    return ((R / P - 1) * C_buf * P + C * P) * es;
+}
+
+}  // namespace
+
+int segblocks_log_probs(const void* logits, int dtype, int layout, int N, int C, int H, int W, int C_buf,
+                        const int64_t* labels, long long ignore, int topk, float* logp, float* lse, float* entropy,
+                        float* top_logp, int32_t* top_index, void* workspace, size_t ws_bytes, hipStream_t stream) {
+    const char* fn = "segblocks_log_probs";
+    sb::LogpArgs a{};
+    int s;
+    if ((s = check_scores(fn, dtype, layout, N, C, H, W, C_buf, topk, &a.R, &a.P))) return s;
+    if (!logits || !lse) return fail(SB_EINVAL, fn, "logits or lse is NULL");
+    if (!labels != !logp) return fail(SB_EINVAL, fn, "labels and logp go together");
+    if ((topk > 0) != (top_logp != nullptr) || (topk > 0) != (top_index != nullptr))
+        return fail(SB_EINVAL, fn, "top_logp and top_index go with topk > 0");
+    a.z = logits;
+    a.labels = (const long long*)labels;
+    a.logp = logp;
+    a.lse = lse;
+    a.entropy = entropy;
+    a.top_logp = top_logp;
+    a.top_index = top_index;
+    a.C_buf = C_buf;
+    a.ignore = ignore;
+    a.C = C;
+    a.topk = topk;
+    const long long f = a.R * 4;
+    const Range rz{logits, scores_bytes(a.R, a.P, C, C_buf, esize(dtype))}, rl{labels, a.R * 8};
+    const std::vector<Range> outs{{logp, f}, {lse, f}, {entropy, f}, {top_logp, f * topk}, {top_index, f * topk}};
+    if (any_overlap(outs, {rz, rl})) return fail(SB_EINVAL, fn, "output buffers overlap inputs or each other");
+    const size_t need = sb::logp_ws_bytes(dtype, a);
+    if ((s = check_ws(fn, need, workspace, ws_bytes))) return s;
+    if (need && any_overlap({{workspace, (long long)need}}, {rz, rl, outs[0], outs[1], outs[2], outs[3], outs[4]}))
+        return fail(SB_EINVAL, fn, "the workspace overlaps an argument");
+    return hip_status(fn, sb::launch_logp(dtype, a, sb::Ws{workspace, need}, stream));
+}
+
+int segblocks_log_probs_workspace_size(int dtype, int layout, int N, int C, int H, int W, int C_buf, int topk,
+                                       size_t* bytes) {
+    const char* fn = "segblocks_log_probs_workspace_size";
+    sb::LogpArgs a{};
+    int s;
+    if (!bytes) return fail(SB_EINVAL, fn, "bytes is NULL");
+    if ((s = check_scores(fn, dtype, layout, N, C, H, W, C_buf, topk, &a.R, &a.P))) return s;
+    a.C = C;
+    a.C_buf = C_buf;
+    a.topk = topk;
+    *bytes = sb::logp_ws_bytes(dtype, a);
+    g_err.clear();
+    return SB_OK;
+}
+
+int segblocks_log_probs_backward(const void* logits, int dtype, int layout, int N, int C, int H, int W, int C_buf,
+                                 const int64_t* labels, long long ignore, const float* lse, const float* d_logp,
+                                 const float* entropy, const float* d_entropy, int topk, const int32_t* top_index,
+                                 const float* d_top, int C_dbuf, void* dlogits, hipStream_t stream) {
+    const char* fn = "segblocks_log_probs_backward";
+    sb::LogpGradArgs a{};
+    int s;
+    if ((s = check_scores(fn, dtype, layout, N, C, H, W, C_buf, topk, &a.R, &a.P)) ||
+        (s = check_scores(fn, dtype, layout, N, C, H, W, C_dbuf, topk, &a.R, &a.P)))
+        return s;
+    if (!logits || !lse || !dlogits) return fail(SB_EINVAL, fn, "logits, lse or dlogits is NULL");
+    if (d_logp && !labels) return fail(SB_EINVAL, fn, "d_logp needs labels");
+    if (d_entropy && !entropy) return fail(SB_EINVAL, fn, "d_entropy needs entropy");
+    if ((topk > 0) != (top_index != nullptr) || (topk > 0) != (d_top != nullptr))
+        return fail(SB_EINVAL, fn, "top_index and d_top go with topk > 0");
+    if (!d_logp && !d_entropy && !d_top) return fail(SB_EINVAL, fn, "no gradient given");
+    a.z = logits;
+    a.dz = dlogits;
+    a.labels = (const long long*)labels;
+    a.lse = lse;
+    a.d_logp = d_logp;
+    a.entropy = entropy;
+    a.d_entropy = d_entropy;
+    a.d_top = d_top;
+    a.top_index = top_index;
+    a.C_buf = C_buf;
+    a.C_dbuf = C_dbuf;
+    a.ignore = ignore;
+    a.C = C;
+    a.topk = topk;
+    const long long f = a.R * 4;
+    const int es = esize(dtype);
+    if (any_overlap({{dlogits, scores_bytes(a.R, a.P, C, C_dbuf, es)}},
+                    {{logits, scores_bytes(a.R, a.P, C, C_buf, es)}, {labels, a.R * 8}, {lse, f}, {d_logp, f},
+                     {entropy, f}, {d_entropy, f}, {top_index, f * topk}, {d_top, f * topk}}))
+        return fail(SB_EINVAL, fn, "dlogits overlaps an input");
+    return hip_status(fn, sb::launch_logp_grad(dtype, a, stream));
+}
+
+namespace {
+
+// Sizes of a list of updates, and its entries as the launcher takes them.
+int check_matrices(const char* fn, const sb_matrix* mats, int count, int dtype, std::vector<sb::OrthMat>& v) {
+    if (dtype != SB_F32 && dtype != SB_F16 && dtype != SB_BF16) return fail(SB_EINVAL, fn, "bad dtype %d", dtype);
+    if (!mats || count <= 0 || count > 4096) return fail(SB_EINVAL, fn, "between 1 and 4096 matrices (got %d)", count);
+    for (int i = 0; i < count; ++i) {
+        const sb_matrix& q = mats[i];
+        if (q.batch <= 0 || q.rows <= 0 || q.cols <= 0)
+            return fail(SB_EINVAL, fn, "batch, rows, cols of entry %d must be positive (got %d, %d, %d)", i, q.batch,
+                        q.rows, q.cols);
+        if (std::min(q.rows, q.cols) > 32768 || std::max(q.rows, q.cols) > (1 << 26) ||
+            (long long)q.rows * q.cols > (1LL << 34) || (long long)q.rows * q.cols * q.batch > (1LL << 36))
+            return fail(SB_ESHAPE, fn, "entry %d is too large (%d x %d x %d)", i, q.batch, q.rows, q.cols);
+        if (q.ld < q.cols || q.ld_out < q.cols)
+            return fail(SB_EINVAL, fn, "rows of entry %d overlap (ld %lld, ld_out %lld for %d columns)", i, q.ld, q.ld_out,
+                        q.cols);
+        const long long one = (q.rows - 1) * q.ld_out + q.cols;
+        if (q.ld > (1LL << 36) || q.ld_out > (1LL << 36) || q.batch_stride < 0 || q.batch_stride > (1LL << 44) ||
+            q.batch_stride_out > (1LL << 44) || (q.batch > 1 && q.batch_stride_out < one))
+            return fail(SB_EINVAL, fn, "bad strides of entry %d", i);
+        v.push_back({q.update, q.out, q.ld, q.ld_out, q.batch > 1 ? q.batch_stride : 0,
+                     q.batch > 1 ? q.batch_stride_out : 0, q.batch, q.rows, q.cols});
+    }
+    return SB_OK;
+}
+
+}  // namespace
+
+int segblocks_orthogonalize(const sb_matrix* matrices, int count, int dtype, int steps, const double* coefficients,
+                            double eps, void* workspace, size_t ws_bytes, hipStream_t stream) {
+    const char* fn = "segblocks_orthogonalize";
+    std::vector<sb::OrthMat> v;
+    int s;
+    if ((s = check_matrices(fn, matrices, count, dtype, v))) return s;
+    if (steps < 1 || steps > 32) return fail(SB_EINVAL, fn, "steps must be in [1, 32] (got %d)", steps);
+    if (!coefficients) return fail(SB_EINVAL, fn, "coefficients is NULL");
+    for (int i = 0; i < 3 * steps; ++i)
+        if (!(fabs(coefficients[i]) <= 1e4)) return fail(SB_EINVAL, fn, "coefficient %d is not in [-1e4, 1e4]", i);
+    if (!(eps >= 0.0) || !(eps <= 1e30)) return fail(SB_EINVAL, fn, "eps must be in [0, 1e30]");
+    const long long es = esize(dtype);
+    std::vector<Range> ins, outs;
+    for (int i = 0; i < count; ++i) {
+        const sb::OrthMat& q = v[(size_t)i];
+        if (!q.g || !q.o) return fail(SB_EINVAL, fn, "update or out of entry %d is NULL", i);
+        ins.push_back({q.g, ((q.batch - 1) * q.bstride + (q.m - 1) * q.ld + q.n) * es});
+        outs.push_back({q.o, ((q.batch - 1) * q.bstride_o + (q.m - 1) * q.ld_o + q.n) * es});
+    }
+    const size_t need = sb::orth_ws_bytes(dtype, v.data(), count);
+    if ((s = check_ws(fn, need, workspace, ws_bytes))) return s;
+    outs.push_back({workspace, (long long)need});
+    if (any_overlap(outs, ins)) return fail(SB_EINVAL, fn, "outputs or the workspace overlap inputs or each other");
+    return hip_status(fn, sb::launch_orth(dtype, v.data(), count, steps, coefficients, eps, sb::Ws{workspace, need},
+                                          stream));
+}
+
+int segblocks_orthogonalize_workspace_size(const sb_matrix* matrices, int count, int dtype, size_t* bytes) {
+    const char* fn = "segblocks_orthogonalize_workspace_size";
+    std::vector<sb::OrthMat> v;
+    int s;
+    if (!bytes) return fail(SB_EINVAL, fn, "bytes is NULL");
+    if ((s = check_matrices(fn, matrices, count, dtype, v))) return s;
+    *bytes = sb::orth_ws_bytes(dtype, v.data(), count);
+    g_err.clear();
+    return SB_OK;
+}
+
 }  // extern "C"

@@ -190,6 +190,44 @@ int policy_max_blocks();
 hipError_t launch_policy(int dtype, int layout, const void* x, int N, int C, int H, int W, int bs, float* score,
                          int khigh, uint8_t* mask, hipStream_t st);
 
+// Log probabilities of class scores and their gradient (sb_logprobs.hip).  A row
+// r = n * P + p holds C classes at z[(n * C_buf + c) * P + p]: P = H * W pixels of
+// a plane for NCHW, P = 1 and n = r otherwise.  The alternatives of a row are
+// at [(n * topk + i) * P + p].  At most logp_max_top() of them.
+struct LogpArgs {
+    const void* z;
+    const long long* labels;  // or nullptr (logp too)
+    float *logp, *lse, *entropy, *top_logp;  // entropy, top_* or nullptr
+    int* top_index;
+    long long R, P, C_buf, ignore;
+    int C, topk;
+};
+struct LogpGradArgs {
+    const void* z;
+    void* dz;  // classes at dz[(n * C_dbuf + c) * P + p]
+    const long long* labels;
+    const float *lse, *d_logp, *entropy, *d_entropy, *d_top;  // d_* or nullptr; labels / entropy / top_index with theirs
+    const int* top_index;
+    long long R, P, C_buf, C_dbuf, ignore;
+    int C, topk;
+};
+int logp_max_top();
+size_t logp_ws_bytes(int dtype, const LogpArgs& a);
+hipError_t launch_logp(int dtype, const LogpArgs& a, Ws ws, hipStream_t st);
+hipError_t launch_logp_grad(int dtype, const LogpGradArgs& a, hipStream_t st);
+
+// Newton-Schulz orthogonalisation (sb_orth.hip): matrices in row-major memory,
+// coefficients a, b, c of every step.
+struct OrthMat {
+    const void* g;
+    void* o;
+    long long ld, ld_o, bstride, bstride_o;  // elements between rows and between matrices of the batch
+    int batch, m, n;
+};
+size_t orth_ws_bytes(int dtype, const OrthMat* mats, int count);
+hipError_t launch_orth(int dtype, const OrthMat* mats, int count, int steps, const double* coef, double eps, Ws ws,
+                       hipStream_t st);
+
 // Persistent convolution with LDS-resident weights (channels-last fp16/bf16,
 // C_in <= 64, blocks of 32 or 64); conv_res_fits tells whether it applies,
 // conv_res_fits_shape the same without the pointer alignment.
