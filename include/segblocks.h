@@ -529,8 +529,8 @@ int segblocks_maxpool_blocks(const void* hi, const void* lo, int dtype, int layo
  * NULL with topk = 0.  A class at -inf has probability 0 and adds nothing to
  * the entropy; a row with every class at -inf has lse, logp and top_logp -inf
  * and entropy 0.  A row that holds NaN or +inf has NaN for lse, logp, entropy
- * and top_logp (NaN ranks above every number).  At most 2^31 - 1 rows and
- * classes.  Needs a workspace where few rows are split over several
+ * and top_logp (NaN ranks above every number).  At most 2^31 - 1 rows of
+ * 2^30 classes.  Needs a workspace where few rows are split over several
  * workgroups: segblocks_log_probs_workspace_size. */
 int segblocks_log_probs(const void* logits, int dtype, int layout, int N, int C, int H, int W, int C_buf,
                         const int64_t* labels, long long ignore, int topk, float* logp, float* lse, float* entropy,

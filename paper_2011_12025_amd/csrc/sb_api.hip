@@ -1067,6 +1067,7 @@ int check_scores(const char* fn, int dtype, int layout, int N, int C, int H, int
     if (layout != SB_NCHW && layout != SB_NHWC) return fail(SB_EINVAL, fn, "bad layout %d", layout);
     if (N <= 0 || C <= 0 || H <= 0 || W <= 0)
         return fail(SB_EINVAL, fn, "N, C, H, W must be positive (got %d, %d, %d, %d)", N, C, H, W);
+    if (C > (1 << 30)) return fail(SB_ESHAPE, fn, "at most 2^30 classes (got %d)", C);
     if (C_buf < C) return fail(SB_EINVAL, fn, "the buffer's channels must hold the classes (got %d for %d)", C_buf, C);
     if (topk < 0 || topk > sb::logp_max_top() || topk > C)
         return fail(SB_EINVAL, fn, "topk must be in [0, min(%d, C)] (got %d)", sb::logp_max_top(), topk);

@@ -11,7 +11,10 @@
 // Gradient, with p_j = exp(z_j - lse) and G the sum of the row's gradients of
 // log probabilities:
 //   dz_j = [j = label] g + sum_i [j = top_i] g_i - p_j (G + g_H (ln p_j + H)).
+#include <limits.h>
 #include <math.h>
+
+#include <algorithm>
 
 #include "sb_common.h"
 #include "sb_kernels.h"
@@ -81,6 +84,7 @@ __device__ __forceinline__ float key_score(u64 k) {
     return __uint_as_float(b == 0xFFFFFFFFu ? 0x7FC00000u : (b & 0x80000000u) ? b ^ 0x80000000u : ~b);
 }
 
+// What a row's results come from.
 struct Row {
     float m, ln_s;  // s = 0 (every class at -inf): an empty row
     bool empty;
@@ -90,114 +94,797 @@ struct Row {
     __device__ __forceinline__ float entropy(const Acc& a) const { return empty ? 0.0f : ln_s - LN2 * a.t / a.s; }
 };
 
-// One 256-thread workgroup a row, class by class; the alternatives one after
-// the other, each the largest key below the one before.
-template <typename T>
-__global__ __launch_bounds__(WG) void k_logp_row(LogpArgs a) {
-    const long long r = blockIdx.x, n = r / a.P, p = r - n * a.P;
-    const T* z = (const T*)a.z + n * a.C_buf * a.P + p;
-    __shared__ Acc s_acc[WG / 64];
-    __shared__ u64 s_key[WG / 64];
-    const int tid = (int)threadIdx.x, lane = lane_id(), wave = tid >> 6;
+// ---------------------------------------------------------------------------
+// A wave's list of alternatives: lane i holds the i-th largest key so far.
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ u64 lane_key(u64 k, int lane) {
+    return (u64)(uint32_t)__builtin_amdgcn_readlane((int)(k >> 32), lane) << 32 |
+           (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)k, lane);
+}
+
+struct TopList {
+    u64 key;    // this lane's
+    u64 last;   // the topk-th
+    float cut;  // its score: below it nothing can enter (NaN while the list has room)
+
+    __device__ __forceinline__ void close(int topk) {
+        last = lane_key(key, topk - 1);
+        cut = last ? key_score(last) : NAN;
+    }
+    // one key a lane (0: none), ranked by counting the larger ones
+    __device__ __forceinline__ void start(u64 k, int topk) {
+        int rank = 0;
+#pragma unroll 8
+        for (int l = 0; l < 64; ++l) {
+            const u64 o = lane_key(k, l);
+            rank += o > k || (o == k && l < lane_id()) ? 1 : 0;
+        }
+        const uint32_t hi = (uint32_t)__builtin_amdgcn_ds_permute(rank * 4, (int)(k >> 32));
+        const uint32_t lo = (uint32_t)__builtin_amdgcn_ds_permute(rank * 4, (int)(uint32_t)k);
+        key = (u64)hi << 32 | lo;
+        close(topk);
+    }
+    // one more key a lane (0: none)
+    __device__ __forceinline__ void offer(u64 k, int topk) {
+        u64 in = __ballot(k > last);
+        while (in) {
+            const int src = __ffsll((unsigned long long)in) - 1;
+            const u64 nk = lane_key(k, src);
+            const u64 up = (u64)(uint32_t)__builtin_amdgcn_update_dpp(-1, (int)(key >> 32), 0x138, 0xF, 0xF, false) << 32 |
+                           (uint32_t)__builtin_amdgcn_update_dpp(-1, (int)(uint32_t)key, 0x138, 0xF, 0xF, false);
+            // (up: the key of the lane below, all ones in lane 0)
+            key = key > nk ? key : up > nk ? nk : up;
+            close(topk);
+            in &= ~(1ull << src);
+            in &= __ballot(k > last);
+        }
+    }
+};
+
+// ---------------------------------------------------------------------------
+// Rows with many classes: NW waves share a row (or one of the parts it is
+// split into), or with NW = 1 each wave of four has a row of its own.  A lane
+// takes 16-byte vectors, U of them in flight, and keeps its own (m, s, t);
+// scores enter the list of alternatives where they pass its last one.
+// ---------------------------------------------------------------------------
+constexpr int LU = 4;
+
+template <typename T> constexpr int LV = 16 / (int)sizeof(T);
+
+struct Part {  // results of a part of a row in the workspace, followed by topk keys
+    float m, s, t, unused;
+};
+__host__ __device__ inline long long part_bytes(int topk) { return 16 + 8LL * topk; }
+
+template <typename T, bool ENT>
+__device__ __forceinline__ void add_vectors(Acc& a, const float (&f)[LU][LV<T>], const float (&vm)[LU]) {
+    float m2 = a.m;
+#pragma unroll
+    for (int u = 0; u < LU; ++u) m2 = fmaxf(m2, vm[u]);
+    raise(a, m2);
+    float s[2] = {}, t[2] = {};
+#pragma unroll
+    for (int u = 0; u < LU; ++u)
+#pragma unroll
+        for (int i = 0; i < LV<T>; ++i) {
+            const float d = (f[u][i] - m2) * LOG2E, e = exp2_(d);  // (NaN stays in e)
+            s[i & 1] += e;
+            if (ENT) t[i & 1] = fmaf(e, fmaxf(d, FAR), t[i & 1]);
+        }
+    a.s += s[0] + s[1];
+    if (ENT) a.t += t[0] + t[1];
+}
+
+template <typename T, int NW, bool TOP, bool ENT>
+__global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void k_logp_rows(LogpArgs a, int parts, char* ws) {
+    constexpr int V = LV<T>, THREADS = NW == 1 ? 256 : NW * 64;
+    __shared__ float s_acc[3][NW];
+    __shared__ u64 s_key[TOP && NW > 1 ? NW * 64 : 1];
+    const int lane = lane_id(), wid = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int wave = NW == 1 ? 0 : wid;
+    const long long item = NW == 1 ? (long long)blockIdx.x * 4 + wid : (long long)blockIdx.x;
+    const long long r = NW == 1 ? item : item / parts;
+    const int part = NW == 1 ? 0 : (int)(item - r * parts);
+    if (r >= a.R) return;  // (NW = 1 alone: whole waves, and no barrier follows)
+    const T* z = (const T*)a.z + r * a.C_buf;
+
+    // [0, head) and [tail, C) score by score, whole vectors between
+    const int head = min(a.C, (int)((16 - (reinterpret_cast<uintptr_t>(z) & 15)) & 15) / (int)sizeof(T));
+    const int nv = (a.C - head) / V, tail = head + nv * V;
+    const int v0 = (int)((long long)nv * part / parts), v1 = (int)((long long)nv * (part + 1) / parts);
+    const T* zv = z + head;
+
     Acc acc = nothing();
-    for (int j = tid; j < a.C; j += WG) add(acc, to_f32(z[j * a.P]));
+    TopList top;
+    bool begun = false;
+    if (TOP) {
+        top.key = 0;
+        top.close(a.topk);
+    }
+    auto one = [&](int j, bool in) {  // a single score a lane
+        const float f = in ? to_f32(z[j]) : -INFINITY;
+        add(acc, f);
+        if (TOP) top.offer(in ? key_of(f, j) : 0, a.topk);
+    };
+    if (part == 0 && wave == 0 && head) one(lane, lane < head);
+
+    typename RawT<16>::type cur[LU], nxt[LU];
+    constexpr int STEP = NW * 64 * LU;
+    auto load = [&](typename RawT<16>::type(&to)[LU], int base) {
+#pragma unroll
+        for (int u = 0; u < LU; ++u) {
+            const int v = base + u * 64 + lane;
+            if (v < v1) to[u] = ld_nt16(zv + (long long)v * V);
+        }
+    };
+    int base = v0 + wave * (64 * LU);
+    if (base < v1) load(cur, base);
+    for (; base < v1; base += STEP) {
+        if (base + STEP < v1) load(nxt, base + STEP);
+        float f[LU][V], vm[LU];
+#pragma unroll
+        for (int u = 0; u < LU; ++u) {
+            Vec<T, V> q;
+            q.raw = cur[u];
+            const bool in = base + u * 64 + lane < v1;
+#pragma unroll
+            for (int i = 0; i < V; ++i) f[u][i] = in ? to_f32(q.e[i]) : -INFINITY;
+            vm[u] = f[u][0];
+#pragma unroll
+            for (int i = 1; i < V; ++i) vm[u] = fmaxf(vm[u], f[u][i]);
+        }
+        add_vectors<T, ENT>(acc, f, vm);
+        if (TOP) {
+            const bool nan = acc.s != acc.s;  // then vm says nothing
+#pragma unroll
+            for (int u = 0; u < LU; ++u) {
+                const int v = base + u * 64 + lane;
+                const bool in = v < v1;
+                const int j = head + v * V;
+                if (__ballot(!(vm[u] <= top.cut) || nan) == 0) continue;
+                u64 own = 0;
+                if (!begun) {  // the list starts as the largest of every lane
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        const u64 k = key_of(f[u][i], j + i);
+                        own = in && k > own ? k : own;
+                    }
+                    if (__ballot(top.key != 0) == 0) top.start(own, a.topk);
+                    else top.offer(own, a.topk);
+                    begun = true;
+                }
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    if (__ballot(!(f[u][i] < top.cut)) == 0) continue;
+                    const u64 k = key_of(f[u][i], j + i);
+                    top.offer(in && k != own ? k : 0, a.topk);
+                }
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < LU; ++u) cur[u] = nxt[u];
+    }
+    if (part == parts - 1 && wave == NW - 1 && tail < a.C) one(tail + lane, tail + lane < a.C);
+
     acc = wave_join(acc);
-    if (lane == 0) s_acc[wave] = acc;
-    __syncthreads();
-    acc = s_acc[0];
-    for (int w = 1; w < WG / 64; ++w) join(acc, s_acc[w]);
+    if (NW > 1) {
+        if (lane == 0) {
+            s_acc[0][wave] = acc.m;
+            s_acc[1][wave] = acc.s;
+            s_acc[2][wave] = acc.t;
+        }
+        if (TOP && lane < a.topk) s_key[wave * a.topk + lane] = top.key;
+        __syncthreads();
+        acc = Acc{s_acc[0][0], s_acc[1][0], s_acc[2][0]};
+        for (int w = 1; w < NW; ++w) join(acc, Acc{s_acc[0][w], s_acc[1][w], s_acc[2][w]});
+    }
+    Part* out = parts > 1 ? (Part*)(ws + item * part_bytes(a.topk)) : nullptr;
     const Row row(acc);
+    const int tid = NW == 1 ? lane : (int)threadIdx.x;
+    auto alternative = [&](int i, u64 k) {
+        if (out) {
+            ((u64*)(out + 1))[i] = k;
+        } else {
+            a.top_logp[r * a.topk + i] = row.logp(key_score(k));
+            a.top_index[r * a.topk + i] = key_class(k);
+        }
+    };
+    if (TOP) {
+        if (NW == 1) {
+            if (lane < a.topk) alternative(lane, top.key);
+        } else {  // the waves' lists: a key's place is the number of larger ones
+            const int n = NW * a.topk;
+            for (int i = tid; i < n; i += THREADS) {
+                const u64 k = s_key[i];
+                int rank = 0;
+                for (int o = 0; o < n; ++o) rank += s_key[o] > k ? 1 : 0;
+                // (a part of fewer classes than topk has keys 0, all behind)
+                if (k ? rank < a.topk : false) alternative(rank, k);
+            }
+            if (out) {
+                int have = 0;
+                for (int o = 0; o < n; ++o) have += s_key[o] != 0 ? 1 : 0;
+                for (int i = have + tid; i < a.topk; i += THREADS) alternative(i, 0);
+            }
+        }
+    }
+    if (tid != 0) return;
+    if (out) {
+        *out = Part{acc.m, acc.s, acc.t, 0.0f};
+        return;
+    }
+    a.lse[r] = row.lse();
+    if (ENT) a.entropy[r] = row.entropy(acc);
+    if (a.labels) {
+        const long long t = a.labels[r];
+        a.logp[r] = t == a.ignore ? 0.0f : t < 0 || t >= a.C ? NAN : row.logp(to_f32(z[t]));
+    }
+}
+
+// The parts of a row, one workgroup a row.
+constexpr int MAX_PARTS = 16;
+template <typename T>
+__global__ __launch_bounds__(256) void k_logp_join(LogpArgs a, int parts, const char* ws) {
+    __shared__ u64 s_key[MAX_PARTS * 64];
+    const long long r = blockIdx.x, pb = part_bytes(a.topk);
+    const char* in = ws + r * parts * pb;
+    const int n = parts * a.topk, tid = (int)threadIdx.x;
+    for (int i = tid; i < n; i += 256) s_key[i] = ((const u64*)(in + i / a.topk * pb + 16))[i % a.topk];
+    __syncthreads();
+    Acc acc = nothing();
+    for (int p = 0; p < parts; ++p) {
+        const Part q = *(const Part*)(in + p * pb);
+        join(acc, Acc{q.m, q.s, q.t});
+    }
+    const Row row(acc);
+    for (int i = tid; i < n; i += 256) {
+        const u64 k = s_key[i];
+        int rank = 0;
+        for (int o = 0; o < n; ++o) rank += s_key[o] > k ? 1 : 0;
+        if (k && rank < a.topk) {
+            a.top_logp[r * a.topk + rank] = row.logp(key_score(k));
+            a.top_index[r * a.topk + rank] = key_class(k);
+        }
+    }
     if (tid == 0) {
         a.lse[r] = row.lse();
         if (a.entropy) a.entropy[r] = row.entropy(acc);
         if (a.labels) {
             const long long t = a.labels[r];
-            a.logp[r] = t == a.ignore ? 0.0f : t < 0 || t >= a.C ? NAN : row.logp(to_f32(z[t * a.P]));
+            a.logp[r] = t == a.ignore ? 0.0f
+                        : t < 0 || t >= a.C ? NAN : row.logp(to_f32(((const T*)a.z)[r * a.C_buf + t]));
         }
-    }
-    u64 last = ~0ull;
-    for (int i = 0; i < a.topk; ++i) {
-        u64 best = 0;
-        for (int j = tid; j < a.C; j += WG) {
-            const u64 k = key_of(to_f32(z[j * a.P]), j);
-            if (k < last && k > best) best = k;
-        }
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) {
-            const u64 k = __shfl_xor(best, o, 64);
-            best = k > best ? k : best;
-        }
-        __syncthreads();
-        if (lane == 0) s_key[wave] = best;
-        __syncthreads();
-        for (int w = 0; w < WG / 64; ++w) best = s_key[w] > best ? s_key[w] : best;
-        if (tid == 0) {
-            const long long q = (n * a.topk + i) * a.P + p;
-            a.top_logp[q] = row.logp(key_score(best));
-            a.top_index[q] = key_class(best);
-        }
-        last = best;
     }
 }
 
-template <typename T>
-__global__ __launch_bounds__(WG) void k_logp_grad_row(LogpGradArgs a) {
-    const long long r = blockIdx.x, n = r / a.P, p = r - n * a.P;
-    const T* z = (const T*)a.z + n * a.C_buf * a.P + p;
-    T* dz = (T*)a.dz + n * a.C_dbuf * a.P + p;
-    float lse = a.lse[r], g = 0.0f;
-    long long label = -1;
-    if (a.d_logp) {
-        label = a.labels[r];
-        if (label == a.ignore) label = -1;
-        else g = label < 0 || label >= a.C ? NAN : a.d_logp[r];
+// ---------------------------------------------------------------------------
+// One thread a row (or a few waves, each with a range of its classes): scores
+// come eight at a time, the alternatives are a sorted list in registers
+// (K <= 8) or in LDS.  Used where rows are short or where neighbouring rows are
+// neighbours in memory (the pixels of a plane).
+// ---------------------------------------------------------------------------
+// Order of two scores as integers; INT_MIN is below all.
+__device__ __forceinline__ int rank_of(float z) {
+    const int b = __float_as_int(z + 0.0f);
+    return z != z ? 0x7FFFFFFF : b ^ ((b >> 31) & 0x7FFFFFFF);
+}
+__device__ __forceinline__ float rank_score(int k) {
+    return k == 0x7FFFFFFF ? NAN : __int_as_float(k ^ ((k >> 31) & 0x7FFFFFFF));
+}
+
+template <int K>
+struct RegTop {  // classes come in rising order: an equal score stays behind
+    int k[K], j[K];
+    __device__ __forceinline__ RegTop(int*, int) {
+#pragma unroll
+        for (int i = 0; i < K; ++i) {
+            k[i] = INT_MIN;
+            j[i] = 0;
+        }
     }
-    const float gh = a.d_entropy ? a.d_entropy[r] : 0.0f, H = a.d_entropy ? a.entropy[r] : 0.0f;
-    auto top = [&](int i) { return (n * a.topk + i) * a.P + p; };
-    float G = g;
-    for (int i = 0; i < a.topk; ++i) {
-        const int j = a.top_index[top(i)];
-        G += j < 0 || j >= a.C ? NAN : a.d_top[top(i)];
+    __device__ __forceinline__ void put(int key, int cls) {
+        if (key > k[K - 1]) {
+#pragma unroll
+            for (int i = K - 1; i > 0; --i) {
+                const bool here = key > k[i], above = key > k[i - 1];
+                k[i] = above ? k[i - 1] : here ? key : k[i];
+                j[i] = above ? j[i - 1] : here ? cls : j[i];
+            }
+            if (key > k[0]) {
+                k[0] = key;
+                j[0] = cls;
+            }
+        }
+    }
+    __device__ __forceinline__ int key(int i) const {
+        int r = k[0];
+#pragma unroll
+        for (int x = 1; x < K; ++x) r = i == x ? k[x] : r;
+        return r;
+    }
+    __device__ __forceinline__ int cls(int i) const {
+        int r = j[0];
+#pragma unroll
+        for (int x = 1; x < K; ++x) r = i == x ? j[x] : r;
+        return r;
+    }
+};
+template <>
+struct RegTop<0> {
+    __device__ __forceinline__ RegTop(int*, int) {}
+    __device__ __forceinline__ void put(int, int) {}
+    __device__ __forceinline__ int key(int) const { return 0; }
+    __device__ __forceinline__ int cls(int) const { return 0; }
+};
+// topk (key, class) pairs of this thread in LDS, 64 words between those of a lane.
+template <>
+struct RegTop<-1> {
+    int* p;
+    int n, last;
+    __device__ __forceinline__ RegTop(int* lds, int topk) : p(lds + lane_id()), n(topk), last(INT_MIN) {
+        for (int i = 0; i < n; ++i) p[128 * i] = INT_MIN;
+    }
+    __device__ __forceinline__ void put(int key, int cls) {
+        if (key <= last) return;
+        int i = n - 1;
+        for (; i > 0 && key > p[128 * (i - 1)]; --i) {
+            p[128 * i] = p[128 * (i - 1)];
+            p[128 * i + 64] = p[128 * (i - 1) + 64];
+        }
+        p[128 * i] = key;
+        p[128 * i + 64] = cls;
+        last = p[128 * (n - 1)];
+    }
+    __device__ __forceinline__ int key(int i) const { return p[128 * i]; }
+    __device__ __forceinline__ int cls(int i) const { return p[128 * i + 64]; }
+};
+__host__ __device__ constexpr int top_lds(int topk) { return 512 * topk; }  // bytes of a wave's lists
+
+template <int K, bool ENT, bool FULL, typename Get>
+__device__ __forceinline__ void scan8(Get get, int c, int c1, Acc& a, RegTop<K>& top) {
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = FULL || c + i < c1 ? get(c + i) : -INFINITY;
+    float m2 = a.m;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m2 = fmaxf(m2, f[i]);
+    raise(a, m2);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if (!FULL && c + i >= c1) break;
+        const float d = (f[i] - m2) * LOG2E, e = exp2_(d);
+        a.s += e;
+        if (ENT) a.t = fmaf(e, fmaxf(d, FAR), a.t);
+        if (K != 0) top.put(rank_of(f[i]), c + i);
+    }
+}
+template <int K, bool ENT, typename Get>
+__device__ __forceinline__ void scan(Get get, int c0, int c1, Acc& a, RegTop<K>& top) {
+    int c = c0;
+    for (; c + 8 <= c1; c += 8) scan8<K, ENT, true>(get, c, c1, a, top);
+    if (c < c1) scan8<K, ENT, false>(get, c, c1, a, top);
+}
+
+// Results of row r = n P + p; zt: the score of its label (where it has one).
+template <int K, bool ENT, typename Get>
+__device__ __forceinline__ void row_out(const LogpArgs& a, long long r, long long n, long long p, const Acc& acc,
+                                        const RegTop<K>& top, Get get) {
+    const Row row(acc);
+    a.lse[r] = row.lse();
+    if (ENT) a.entropy[r] = row.entropy(acc);
+    if (a.labels) {
+        const long long t = a.labels[r];
+        a.logp[r] = t == a.ignore ? 0.0f : t < 0 || t >= a.C ? NAN : row.logp(get((int)t));
+    }
+    if (K != 0)
+        for (int i = 0; i < a.topk; ++i) {
+            const long long q = (n * a.topk + i) * a.P + p;
+            a.top_logp[q] = row.logp(rank_score(top.key(i)));
+            a.top_index[q] = top.cls(i);
+        }
+}
+
+// Where byte f of staged rows lies in LDS: 16 bytes of room after every 128, so
+// that rows at distances which are multiples of the banks do not collide.
+__device__ __forceinline__ int staged(int f) { return f + (f >> 7 << 4); }
+__host__ __device__ constexpr int staged_bytes(int n) { return n + n / 128 * 16 + 16; }
+
+// The first n elements from src, as they lie there, to LDS (all threads).
+template <typename T>
+__device__ __forceinline__ void stage_in(const T* src, int n, char* lds) {
+    constexpr int V = LV<T>;
+    const int tid = (int)threadIdx.x, nt = (int)blockDim.x;
+    if ((reinterpret_cast<uintptr_t>(src) & 15) == 0) {
+        const int nv = n / V;
+        for (int v = tid; v < nv; v += nt) *(uint4*)(lds + staged(v * 16)) = ld_nt16(src + (long long)v * V);
+        for (int e = nv * V + tid; e < n; e += nt) *(T*)(lds + staged(e * (int)sizeof(T))) = src[e];
+    } else {
+        for (int e = tid; e < n; e += nt) *(T*)(lds + staged(e * (int)sizeof(T))) = src[e];
+    }
+}
+
+// Short rows (NHWC, tokens): a workgroup stages blockDim rows as they lie and
+// each thread goes through one.
+template <typename T, int K, bool ENT>
+__global__ __launch_bounds__(256) void k_logp_short(LogpArgs a, int lists) {
+    extern __shared__ __align__(16) char lds[];
+    const int tid = (int)threadIdx.x, rows = (int)blockDim.x;
+    const long long r0 = (long long)blockIdx.x * rows;
+    const int nr = (int)min((long long)rows, a.R - r0), ld = (int)a.C_buf;
+    stage_in((const T*)a.z + r0 * ld, (nr - 1) * ld + a.C, lds + lists);
+    __syncthreads();
+    if (tid >= nr) return;
+    const int at = tid * ld * (int)sizeof(T);
+    auto get = [&](int c) { return to_f32(*(const T*)(lds + lists + staged(at + c * (int)sizeof(T)))); };
+    Acc acc = nothing();
+    RegTop<K> top((int*)(lds + (tid >> 6) * top_lds(a.topk)), a.topk);
+    scan<K, ENT>(get, 0, a.C, acc, top);
+    row_out<K, ENT>(a, r0 + tid, r0 + tid, 0, acc, top, get);
+}
+
+// Pixels of planes (NCHW): 64 neighbouring pixels a wave; NW waves share them
+// and split the classes, so that small maps fill the chip too.
+template <typename T, int K, bool ENT, int NW>
+__global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void k_logp_planes(LogpArgs a, int lists) {
+    extern __shared__ __align__(16) char lds[];  // lists, then the waves' results
+    const int lane = lane_id(), wid = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int wave = NW == 1 ? 0 : wid;
+    const long long r = ((long long)blockIdx.x * (NW == 1 ? 4 : 1) + (NW == 1 ? wid : 0)) * 64 + lane;
+    const bool in = r < a.R;
+    const long long rr = in ? r : a.R - 1, n = rr / a.P, p = rr - n * a.P;
+    const T* z = (const T*)a.z + n * a.C_buf * a.P + p;
+    auto get = [&](int c) { return to_f32(z[c * a.P]); };
+    Acc acc = nothing();
+    RegTop<K> top((int*)(lds + wid * top_lds(a.topk)), a.topk);
+    scan<K, ENT>(get, (int)((long long)a.C * wave / NW), (int)((long long)a.C * (wave + 1) / NW), acc, top);
+    if constexpr (NW > 1) {
+        float* res = (float*)(lds + lists);  // [wave][3][64]
+        int* keys = (int*)(res + NW * 192);  // [wave][topk][2][64] of register lists
+        res[wave * 192 + lane] = acc.m;
+        res[wave * 192 + 64 + lane] = acc.s;
+        res[wave * 192 + 128 + lane] = acc.t;
+        if (K > 0)
+#pragma unroll
+            for (int i = 0; i < (K > 0 ? K : 1); ++i)
+                if (i < a.topk) {
+                    keys[((wave * a.topk + i) * 2) * 64 + lane] = top.key(i);
+                    keys[((wave * a.topk + i) * 2 + 1) * 64 + lane] = top.cls(i);
+                }
+        __syncthreads();
+        if (wave != 0) return;
+        for (int w = 1; w < NW; ++w) {
+            join(acc, Acc{res[w * 192 + lane], res[w * 192 + 64 + lane], res[w * 192 + 128 + lane]});
+            if (K != 0)
+                for (int i = 0; i < a.topk; ++i) {
+                    const int* q = K > 0 ? keys + ((w * a.topk + i) * 2) * 64 + lane
+                                         : (const int*)(lds + w * top_lds(a.topk)) + 128 * i + lane;
+                    if (q[0] != INT_MIN) top.put(q[0], q[64]);
+                }
+        }
+    }
+    if (in) row_out<K, ENT>(a, r, n, p, acc, top, get);
+}
+
+// ---------------------------------------------------------------------------
+// Gradient
+// ---------------------------------------------------------------------------
+struct GradRow {
+    float m, ln_s, g, G, gh, H;
+    long long label;  // -1: none
+    bool empty;
+
+    __device__ __forceinline__ GradRow(const LogpGradArgs& a, long long r, long long n, long long p) {
+        m = a.lse[r];
+        ln_s = 0.0f;
+        empty = m == -INFINITY;
+        g = 0.0f;
+        label = -1;
+        if (a.d_logp) {
+            label = a.labels[r];
+            if (label == a.ignore) label = -1;
+            else g = label < 0 || label >= a.C ? NAN : a.d_logp[r];
+        }
+        gh = a.d_entropy ? a.d_entropy[r] : 0.0f;
+        H = a.d_entropy ? a.entropy[r] : 0.0f;
+        G = g;
+        for (int i = 0; i < a.topk; ++i) {
+            const long long q = (n * a.topk + i) * a.P + p;
+            const int j = a.top_index[q];
+            G += j < 0 || j >= a.C ? NAN : a.d_top[q];
+        }
     }
     // p from lse is off by |lse| 2^-25: past 256 it comes from the row's own maximum
-    float m = lse, ln_s = 0.0f;
-    if (fabsf(lse) > 256.0f && lse != -INFINITY) {
-        Acc acc = nothing();
-        for (int j = 0; j < a.C; ++j) add(acc, to_f32(z[j * a.P]));
+    __device__ __forceinline__ bool far() const { return !empty && !(fabsf(m) <= 256.0f); }
+    __device__ __forceinline__ void take(const Acc& acc) {
         const Row row(acc);
         m = row.m;
         ln_s = row.ln_s;
     }
-    for (int j = (int)threadIdx.x; j < a.C; j += WG) {
-        const float lp = (to_f32(z[j * a.P]) - m) - ln_s, pr = exp2_(lp * LOG2E);
-        float d = -pr * (G + gh * (fmaxf(lp, FAR) + H));
-        if (j == label) d += g;
-        for (int i = 0; i < a.topk; ++i)
-            if (a.top_index[top(i)] == j) d += a.d_top[top(i)];
-        dz[j * a.P] = from_f32<T>(lse == -INFINITY ? 0.0f : d);
+    // what every class gets
+    __device__ __forceinline__ float all(float z) const {
+        const float lp = (z - m) - ln_s, pr = exp2_(lp * LOG2E);
+        const float d = -pr * (G + gh * (fmaxf(lp, FAR) + H));
+        return empty ? 0.0f : d;
     }
+    // and the label's class or an alternative's in full
+    __device__ __forceinline__ float at(const LogpGradArgs& a, float z, int j, long long n, long long p) const {
+        float d = all(z);
+        if (empty) return d;
+        if (j == label) d += g;
+        for (int i = 0; i < a.topk; ++i) {
+            const long long q = (n * a.topk + i) * a.P + p;
+            if (a.top_index[q] == j) d += a.d_top[q];
+        }
+        return d;
+    }
+};
+
+// A range of a long row a workgroup.
+template <typename T>
+__global__ __launch_bounds__(256) void k_logp_grad_rows(LogpGradArgs a, int chunks, int per) {
+    constexpr int V = LV<T>;
+    const long long r = blockIdx.x / (unsigned)chunks;
+    const int chunk = (int)(blockIdx.x - (unsigned)r * chunks), tid = (int)threadIdx.x;
+    const T* z = (const T*)a.z + r * a.C_buf;
+    T* dz = (T*)a.dz + r * a.C_dbuf;
+    GradRow row(a, r, r, 0);
+    if (row.far()) {
+        __shared__ float s[3][4];
+        Acc acc = nothing();
+        for (int j = tid; j < a.C; j += 256) add(acc, to_f32(z[j]));
+        acc = wave_join(acc);
+        if (lane_id() == 0) {
+            s[0][tid >> 6] = acc.m;
+            s[1][tid >> 6] = acc.s;
+            s[2][tid >> 6] = acc.t;
+        }
+        __syncthreads();
+        acc = Acc{s[0][0], s[1][0], s[2][0]};
+        for (int w = 1; w < 4; ++w) join(acc, Acc{s[0][w], s[1][w], s[2][w]});
+        row.take(acc);
+    }
+    // vectors where both rows begin alike
+    const int mis = (int)(reinterpret_cast<uintptr_t>(dz) & 15);
+    const bool vec = mis == (int)(reinterpret_cast<uintptr_t>(z) & 15);
+    const int head = vec ? min(a.C, ((16 - mis) & 15) / (int)sizeof(T)) : a.C;
+    const int nv = (a.C - head) / V, tail = head + nv * V;
+    const int c0 = chunk * per, c1 = min(a.C, c0 + per);
+    auto single = [&](int j0, int j1) {
+        for (int j = max(j0, c0) + tid; j < min(j1, c1); j += 256) dz[j] = from_f32<T>(row.all(to_f32(z[j])));
+    };
+    single(0, head);
+    single(tail, a.C);
+    // the vectors that begin in [c0, c1)
+    const int v0 = min(nv, max(0, (c0 - head + V - 1) / V)), v1 = min(nv, max(0, (c1 - head + V - 1) / V));
+    const int vs = c0 <= head ? 0 : v0;
+#pragma unroll 4
+    for (int v = vs + tid; v < v1; v += 256) {
+        Vec<T, V> q, o;
+        q.raw = ld_nt16(z + head + (long long)v * V);
+#pragma unroll
+        for (int i = 0; i < V; ++i) o.e[i] = from_f32<T>(row.all(to_f32(q.e[i])));
+        st_nt16(dz + head + (long long)v * V, o.raw);
+    }
+    // the label's class and the alternatives again, once the rest is written
+    __syncthreads();
+    if (tid <= a.topk) {
+        const long long j = tid < a.topk ? a.top_index[r * a.topk + tid] : row.label;
+        // (the workgroup that wrote it: a vector belongs to the range it begins in)
+        const long long first = j < head || j >= tail ? j : head + (j - head) / V * V;
+        if (j >= 0 && j < a.C && first >= c0 && first < c1) dz[j] = from_f32<T>(row.at(a, to_f32(z[j]), (int)j, r, 0));
+    }
+}
+
+// Short rows, as k_logp_short: gradients go through LDS too, at `out`.
+template <typename T>
+__global__ __launch_bounds__(256) void k_logp_grad_short(LogpGradArgs a, int out) {
+    extern __shared__ __align__(16) char lds[];
+    const int tid = (int)threadIdx.x, rows = (int)blockDim.x;
+    const long long r0 = (long long)blockIdx.x * rows;
+    const int nr = (int)min((long long)rows, a.R - r0), ld = (int)a.C_buf;
+    stage_in((const T*)a.z + r0 * ld, (nr - 1) * ld + a.C, lds);
+    __syncthreads();
+    if (tid < nr) {
+        const long long r = r0 + tid;
+        const int at = tid * ld * (int)sizeof(T), to = tid * a.C * (int)sizeof(T);
+        auto get = [&](int c) { return to_f32(*(const T*)(lds + staged(at + c * (int)sizeof(T)))); };
+        auto put = [&](int c, float v) { *(T*)(lds + out + staged(to + c * (int)sizeof(T))) = from_f32<T>(v); };
+        GradRow row(a, r, r, 0);
+        if (row.far()) {
+            Acc acc = nothing();
+            RegTop<0> none(nullptr, 0);
+            scan<0, false>(get, 0, a.C, acc, none);
+            row.take(acc);
+        }
+#pragma unroll 4
+        for (int c = 0; c < a.C; ++c) put(c, row.all(get(c)));
+        if (row.label >= 0 && row.label < a.C) put((int)row.label, row.at(a, get((int)row.label), (int)row.label, r, 0));
+        for (int i = 0; i < a.topk; ++i) {
+            const int j = a.top_index[r * a.topk + i];
+            if (j >= 0 && j < a.C) put(j, row.at(a, get(j), j, r, 0));
+        }
+    }
+    __syncthreads();
+    T* dz = (T*)a.dz + r0 * a.C_dbuf;
+    const int n = nr * a.C;
+    auto held = [&](int e) { return *(const T*)(lds + out + staged(e * (int)sizeof(T))); };
+    if (a.C_dbuf == a.C && (reinterpret_cast<uintptr_t>(dz) & 15) == 0) {
+        constexpr int V = LV<T>;
+        const int nv = n / V;
+        for (int v = tid; v < nv; v += rows) st_nt16(dz + (long long)v * V, *(const uint4*)(lds + out + staged(v * 16)));
+        for (int e = nv * V + tid; e < n; e += rows) dz[e] = held(e);
+    } else {
+        for (int e = tid; e < n; e += rows) {
+            const int q = e / a.C;
+            dz[q * a.C_dbuf + (e - q * a.C)] = held(e);
+        }
+    }
+}
+
+// Pixels of planes: a thread a pixel and range of classes.
+template <typename T>
+__global__ __launch_bounds__(256) void k_logp_grad_planes(LogpGradArgs a, int per) {
+    const long long r = (long long)blockIdx.x * 256 + threadIdx.x;
+    if (r >= a.R) return;
+    const long long n = r / a.P, p = r - n * a.P;
+    const T* z = (const T*)a.z + n * a.C_buf * a.P + p;
+    T* dz = (T*)a.dz + n * a.C_dbuf * a.P + p;
+    const int c0 = (int)blockIdx.y * per, c1 = min(a.C, c0 + per);
+    auto get = [&](int c) { return to_f32(z[c * a.P]); };
+    GradRow row(a, r, n, p);
+    if (row.far()) {
+        Acc acc = nothing();
+        RegTop<0> none(nullptr, 0);
+        scan<0, false>(get, 0, a.C, acc, none);
+        row.take(acc);
+    }
+#pragma unroll 8
+    for (int c = c0; c < c1; ++c) dz[c * a.P] = from_f32<T>(row.all(get(c)));
+    auto again = [&](long long j) {
+        if (j >= c0 && j < c1) dz[j * a.P] = from_f32<T>(row.at(a, get((int)j), (int)j, n, p));
+    };
+    again(row.label);
+    for (int i = 0; i < a.topk; ++i) again(a.top_index[(n * a.topk + i) * a.P + p]);
+}
+
+// ---------------------------------------------------------------------------
+// Host side
+// ---------------------------------------------------------------------------
+// Rows for one thread each: short ones, staged as they lie (with the channels
+// of the buffer that are no classes).  Returns rows of a workgroup, or 0.
+int short_rows(int es, long long R, int C, long long ld, bool grad) {
+    if (ld > 2LL * C || C > 1024 || (C > 64 && R < 16384)) return 0;
+    for (int rows = 256; rows >= 64; rows /= 2)
+        if (staged_bytes((int)std::min<long long>(rows * ld * es, 1 << 20)) + (grad ? staged_bytes(rows * C * es) : 0) <=
+            (rows == 64 ? 48 : 24) * 1024)
+            return rows;
+    return 0;
+}
+
+int row_waves(long long R, int C) { return C <= 1024 ? 1 : C <= 16384 || R >= 512 ? 4 : 16; }
+
+// Parts of a long row where the rows alone leave most of the chip idle.
+int row_parts(long long R, int C) {
+    if (C < 65536 || R >= 64) return 1;
+    return (int)std::min<long long>({MAX_PARTS, C / 16384, 256 / R});
+}
+
+bool is_planes(long long P) { return P > 1; }
+
+template <typename T, int K>
+hipError_t logp_k(const LogpArgs& a, hipStream_t st, int rows, bool planes) {
+    const bool ent = a.entropy != nullptr;
+    const int es = sizeof(T);
+    if (!planes) {
+        const int lists = K < 0 ? rows / 64 * top_lds(a.topk) : 0;
+        const int lds = lists + staged_bytes(((rows - 1) * (int)a.C_buf + a.C) * es + 16);
+        const unsigned grid = (unsigned)((a.R + rows - 1) / rows);
+        auto run = [&](auto kernel) -> hipError_t {
+            if (lds > 64 * 1024)
+                if (hipError_t e = ensure_dyn_lds((const void*)kernel, lds); e != hipSuccess) return e;
+            hipLaunchKernelGGL(kernel, dim3(grid), dim3(rows), lds, st, a, lists);
+            return hipGetLastError();
+        };
+        return ent ? run(k_logp_short<T, K, true>) : run(k_logp_short<T, K, false>);
+    }
+    // waves that share 64 pixels: until there are eight waves a SIMD or so
+    const long long waves = (a.R + 63) / 64;
+    const int nw = waves >= 4096 || a.C < 32 ? 1 : waves >= 1024 || a.C < 128 ? 4 : 16;
+    auto run = [&](auto kernel, int w) -> hipError_t {
+        const int all = w == 1 ? 4 : w;
+        const int lists = K < 0 ? all * top_lds(a.topk) : 0;
+        const int lds = lists + (w > 1 ? w * 768 + (K > 0 ? w * a.topk * 512 : 0) : 0);
+        const unsigned grid = (unsigned)(w == 1 ? (waves + 3) / 4 : waves);
+        if (lds > 64 * 1024)
+            if (hipError_t e = ensure_dyn_lds((const void*)kernel, lds); e != hipSuccess) return e;
+        hipLaunchKernelGGL(kernel, dim3(grid), dim3(all * 64), lds, st, a, lists);
+        return hipGetLastError();
+    };
+    // (lists of 64 alternatives take 32 KB a wave: four waves at most)
+    if (nw == 16 && !(K < 0 && a.topk > 16))
+        return ent ? run(k_logp_planes<T, K, true, 16>, 16) : run(k_logp_planes<T, K, false, 16>, 16);
+    if (nw >= 4) return ent ? run(k_logp_planes<T, K, true, 4>, 4) : run(k_logp_planes<T, K, false, 4>, 4);
+    return ent ? run(k_logp_planes<T, K, true, 1>, 1) : run(k_logp_planes<T, K, false, 1>, 1);
+}
+
+template <typename T, int NW>
+hipError_t logp_rows(const LogpArgs& a, Ws ws, hipStream_t st, int parts) {
+    const long long items = NW == 1 ? (a.R + 3) / 4 : a.R * parts;
+    const dim3 grid((unsigned)items), block(NW == 1 ? 256 : NW * 64);
+    auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, a, parts, (char*)ws.p); };
+    if (a.topk) a.entropy ? run(k_logp_rows<T, NW, true, true>) : run(k_logp_rows<T, NW, true, false>);
+    else a.entropy ? run(k_logp_rows<T, NW, false, true>) : run(k_logp_rows<T, NW, false, false>);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t logp_t(const LogpArgs& a, Ws ws, hipStream_t st) {
+    const bool planes = is_planes(a.P);
+    const int rows = planes ? 0 : short_rows(sizeof(T), a.R, a.C, a.C_buf, false);
+    if (planes || (rows && (a.topk <= 8 || rows / 64 * top_lds(a.topk) <= 64 * 1024))) {
+        if (a.topk == 0) return logp_k<T, 0>(a, st, rows, planes);
+        if (a.topk == 1) return logp_k<T, 1>(a, st, rows, planes);
+        if (a.topk <= 4) return logp_k<T, 4>(a, st, rows, planes);
+        if (a.topk <= 8) return logp_k<T, 8>(a, st, rows, planes);
+        return logp_k<T, -1>(a, st, rows, planes);
+    }
+    const int parts = row_parts(a.R, a.C);
+    if (parts > 1) {
+        const hipError_t e = logp_rows<T, 4>(a, ws, st, parts);
+        if (e != hipSuccess) return e;
+        hipLaunchKernelGGL(k_logp_join<T>, dim3((unsigned)a.R), dim3(256), 0, st, a, parts, (const char*)ws.p);
+        return hipGetLastError();
+    }
+    const int nw = row_waves(a.R, a.C);
+    if (nw == 1) return logp_rows<T, 1>(a, ws, st, 1);
+    return nw == 4 ? logp_rows<T, 4>(a, ws, st, 1) : logp_rows<T, 16>(a, ws, st, 1);
+}
+
+template <typename T>
+hipError_t grad_t(const LogpGradArgs& a, hipStream_t st) {
+    if (is_planes(a.P)) {
+        const long long wgs = (a.R + 255) / 256;
+        // ranges of classes until there are eight workgroups a CU
+        const int ranges = (int)std::max(1LL, std::min<long long>(2048 / wgs, a.C / 16));
+        const int per = (a.C + ranges - 1) / ranges;
+        hipLaunchKernelGGL(k_logp_grad_planes<T>, dim3((unsigned)wgs, (a.C + per - 1) / per), dim3(256), 0, st, a, per);
+        return hipGetLastError();
+    }
+    if (const int rows = short_rows(sizeof(T), a.R, a.C, a.C_buf, true)) {
+        const int es = sizeof(T), out = (staged_bytes(((rows - 1) * (int)a.C_buf + a.C) * es + 16) + 15) / 16 * 16;
+        const int lds = out + staged_bytes(rows * a.C * es + 16);
+        if (lds > 64 * 1024)
+            if (hipError_t e = ensure_dyn_lds((const void*)k_logp_grad_short<T>, lds); e != hipSuccess) return e;
+        hipLaunchKernelGGL(k_logp_grad_short<T>, dim3((unsigned)((a.R + rows - 1) / rows)), dim3(rows), lds, st, a, out);
+        return hipGetLastError();
+    }
+    // ranges of 4 vectors a thread, or 16 where rows are many
+    int per = 256 * LV<T> * (a.R * a.C >= (64LL << 20) ? 16 : 4);
+    while (a.R * ((a.C + per - 1) / per) >= (1LL << 31)) per *= 2;
+    const int chunks = (a.C + per - 1) / per;
+    hipLaunchKernelGGL(k_logp_grad_rows<T>, dim3((unsigned)(a.R * chunks)), dim3(256), 0, st, a, chunks, per);
+    return hipGetLastError();
 }
 
 }  // namespace
 
 int logp_max_top() { return 64; }
 
-size_t logp_ws_bytes(int, const LogpArgs&) { return 0; }
+size_t logp_ws_bytes(int dtype, const LogpArgs& a) {
+    const int es = dtype == 0 ? 4 : 2;
+    if (is_planes(a.P) || short_rows(es, a.R, a.C, a.C_buf, false)) return 0;
+    const int parts = row_parts(a.R, a.C);
+    return parts > 1 ? (size_t)(a.R * parts * part_bytes(a.topk)) : 0;
+}
 
-hipError_t launch_logp(int dtype, const LogpArgs& a, Ws, hipStream_t st) {
-    const dim3 grid((unsigned)a.R), block(WG);
-    if (dtype == 0) hipLaunchKernelGGL(k_logp_row<float>, grid, block, 0, st, a);
-    else if (dtype == 1) hipLaunchKernelGGL(k_logp_row<f16>, grid, block, 0, st, a);
-    else hipLaunchKernelGGL(k_logp_row<bf16>, grid, block, 0, st, a);
-    return hipGetLastError();
+hipError_t launch_logp(int dtype, const LogpArgs& a, Ws ws, hipStream_t st) {
+    if (dtype == 0) return logp_t<float>(a, ws, st);
+    return dtype == 1 ? logp_t<f16>(a, ws, st) : logp_t<bf16>(a, ws, st);
 }
 
 hipError_t launch_logp_grad(int dtype, const LogpGradArgs& a, hipStream_t st) {
-    const dim3 grid((unsigned)a.R), block(WG);
-    if (dtype == 0) hipLaunchKernelGGL(k_logp_grad_row<float>, grid, block, 0, st, a);
-    else if (dtype == 1) hipLaunchKernelGGL(k_logp_grad_row<f16>, grid, block, 0, st, a);
-    else hipLaunchKernelGGL(k_logp_grad_row<bf16>, grid, block, 0, st, a);
-    return hipGetLastError();
+    if (dtype == 0) return grad_t<float>(a, st);
+    return dtype == 1 ? grad_t<f16>(a, st) : grad_t<bf16>(a, st);
 }
 
 }  // namespace sb
