@@ -18,7 +18,7 @@
 // X but the first are pairs of fp16 numbers hi + lo (22 bits and a sign) times
 // a power of two known beforehand from the polynomial's bounds; a product of
 // two is three MFMAs hi hi + hi lo + lo hi with fp32 sums.  The first X is one
-// fp16 number for 16-bit updates (their values times a power of two; bf16
+// fp16 number for 16-bit updates (fp16 as it is, bf16 times a power of two:
 // values below 2^-38 of the largest are cut) and a pair for fp32.
 #include <math.h>
 
@@ -50,7 +50,9 @@ struct OMat {
     char* ws;        // of the first matrix; the next one's is ws_one bytes on
     long long ws_one;
     int batch, m, n, s, L, sp, Lp;  // sp, Lp: s, L rounded up to whole tiles (zeros)
-    int splits;                     // of the product over L
+    int parts, unit0;               // of X X^T: workgroups of a tile, and the number of the entry's first one
+    int scaled;                     // whether X is the update times a power of two (else as it is)
+    int vec;                        // whether rows of the update / of the result are 16-byte aligned (bits 0 / 1)
 };
 struct Table {
     OMat mat[OM];
@@ -60,8 +62,8 @@ struct Table {
 
 // The workspace of one matrix, in bytes from its start.
 constexpr int MAXP = 1024;  // workgroups that make X, each with its sum of squares
-constexpr int MAXA = 256;   // workgroups that look for the largest value
-constexpr long long W_SUM = 1024, W_X = W_SUM + 4 * MAXP;  // [0]: the largest values
+constexpr int MAXA = 1024;  // workgroups that look for the largest value
+constexpr long long W_SUM = 4 * MAXA, W_X = W_SUM + 4 * MAXP;  // [0]: the largest values
 __host__ __device__ inline long long w_x_bytes(int sp, int Lp) { return (long long)sp * Lp * 4; }
 __host__ __device__ inline long long w_xt(int sp, int Lp, int i) { return W_X + (1 + i) * w_x_bytes(sp, Lp); }
 __host__ __device__ inline long long w_sym(int sp, int Lp, int i) {
@@ -72,19 +74,28 @@ constexpr int SYMS = 5;  // A, T and three that P and Q take in turn
 struct Place {  // of a workgroup
     int mat, b, t;  // entry, matrix of its batch, tile
 };
+// Workgroups go to the eight XCDs in turn; of every entry an XCD gets a run of
+// neighbouring tiles, which share panels, since each L2 fetches for itself what
+// it reads.  (Of every entry and not of the launch: they take unequal time.)
+__device__ __forceinline__ int xcd_run(int k, int n) {
+    const int x = k & 7, q = n >> 3, r = n & 7;
+    return x * q + min(x, r) + (k >> 3);
+}
 template <typename F>  // per_of: workgroups of one matrix of an entry
-__device__ __forceinline__ Place place(const Table& tb, F per_of) {
-    const int bid = (int)blockIdx.x, l = lane_id();
+__device__ __forceinline__ Place place(const Table& tb, F per_of, int bid) {
+    const int l = lane_id();
     const int i = __popcll(__ballot(l < tb.count && bid >= tb.start[min(l, OM)])) - 1;
-    const int t = bid - tb.start[i], per = per_of(tb.mat[i]);
+    const int t = xcd_run(bid - tb.start[i], tb.start[i + 1] - tb.start[i]), per = per_of(tb.mat[i]);
     return Place{i, t / per, t % per};
 }
 
-__device__ __forceinline__ int amax_wgs(const OMat& q) {
-    return (int)min((long long)MAXA, ((long long)q.m * q.n + 16383) / 16384);
+__host__ __device__ inline int amax_wgs(const OMat& q) {
+    const long long n = ((long long)q.m * q.n + 4095) / 4096;
+    return n < MAXA ? (int)n : MAXA;
 }
-__device__ __forceinline__ int prep_wgs(const OMat& q) {
-    return (int)min((long long)MAXP, (long long)(q.sp / 64) * (q.Lp / 64));
+__host__ __device__ inline int prep_wgs(const OMat& q) {
+    const long long n = (long long)(q.sp / 64) * (q.Lp / 64);
+    return n < MAXP ? (int)n : MAXP;
 }
 
 // ---------------------------------------------------------------------------
@@ -115,17 +126,23 @@ __device__ __forceinline__ void store8(char* row, long long k, const float (&v)[
     if (NP == 2) vstore<f16, 8>((f16*)(p + 64), lo);
 }
 
-// A T x T tile in LDS (fp32, rows CP<T> apart) to rows r0.. and columns c0.. of a
-// matrix with K columns; turned: its transpose.
+// An R x T piece in LDS (fp32, rows CP<T> apart) to rows r0.. and columns c0.. of a
+// matrix with K columns; TURNED: its transpose.
 template <int T> constexpr int CP = T + 1;
 
-template <int T, int NP>
-__device__ __forceinline__ void store_tile(const float* C, char* dst, long long K, int r0, int c0, bool turned) {
-    for (int e = (int)threadIdx.x; e < T * T / 8; e += WG) {
-        const int r = e / (T / 8), k = (e % (T / 8)) * 8;
+// Threads of a workgroup with tiles of side T: one wave a SIMD stands still for its
+// own instructions and LDS reads where tiles of 64 are a CU's only one, so those
+// have two, each with half of a stage's K (s = 512: 12.4 -> 11.0 us a product).
+template <int T> constexpr int NT = T == 64 ? 512 : 256;
+
+template <int T, int NP, bool TURNED, int R = T, int THREADS = NT<T>>
+__device__ __forceinline__ void store_tile(const float* C, char* dst, long long K, int r0, int c0) {
+    constexpr int W = (TURNED ? R : T) / 8;  // eights of a stored row
+    for (int e = (int)threadIdx.x; e < R * T / 8; e += THREADS) {
+        const int r = e / W, k = (e % W) * 8;
         float v[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = turned ? C[(k + i) * CP<T> + r] : C[r * CP<T> + k + i];
+        for (int i = 0; i < 8; ++i) v[i] = TURNED ? C[(k + i) * CP<T> + r] : C[r * CP<T> + k + i];
         store8<NP>(dst + (long long)(r0 + r) * K * (2 * NP), c0 + k, v);
     }
 }
@@ -135,63 +152,80 @@ __device__ __forceinline__ void store_tile(const float* C, char* dst, long long 
 // ---------------------------------------------------------------------------
 template <typename T>
 __global__ __launch_bounds__(WG) void k_orth_amax(Table tb) {
+    constexpr int V = 16 / (int)sizeof(T);
     __shared__ float s[WG / 64];
-    const Place p = place(tb, [](const OMat& q) { return amax_wgs(q); });
+    const Place p = place(tb, [](const OMat& q) { return amax_wgs(q); }, (int)blockIdx.x);
     const OMat& q = tb.mat[p.mat];
     const T* g = (const T*)q.g + p.b * q.bstride;
-    const int wave = (int)threadIdx.x >> 6, l = lane_id(), all = amax_wgs(q) * (WG / 64);
+    const int tid = (int)threadIdx.x, l = lane_id(), wgs = amax_wgs(q);
     float m = 0.0f;
-    for (int r = p.t * (WG / 64) + wave; r < q.m; r += all)
-        for (int c = l; c < q.n; c += 64) m = fmaxf(m, fabsf(to_f32(g[r * q.ld + c])));
+    // rows of vectors, or one row of all where nothing lies between them
+    const bool flat = q.ld == q.n;
+    const long long cols = flat ? (long long)q.m * q.n : q.n, rows = flat ? 1 : q.m;
+    const long long nv = q.vec & 1 ? cols / V : 0, all = (long long)wgs * WG;
+    for (long long r = 0; r < rows; ++r) {
+        const T* row = g + r * q.ld;
+#pragma unroll 4
+        for (long long v = (long long)p.t * WG + tid; v < nv; v += all) {
+            Vec<T, V> x;
+            x.raw = *reinterpret_cast<const uint4*>(row + v * V);
+#pragma unroll
+            for (int i = 0; i < V; ++i) m = fmaxf(m, fabsf(to_f32(x.e[i])));
+        }
+#pragma unroll 4
+        for (long long c = nv * V + (long long)p.t * WG + tid; c < cols; c += all) m = fmaxf(m, fabsf(to_f32(row[c])));
+    }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-    if (l == 0) s[wave] = m;
+    if (l == 0) s[tid >> 6] = m;
     __syncthreads();
-    if (threadIdx.x == 0) ((float*)(q.ws + p.b * q.ws_one))[p.t] = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
+    if (tid == 0) ((float*)(q.ws + p.b * q.ws_one))[p.t] = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
 }
 
-// The sum of n floats (fixed order) or their maximum, over a workgroup.
+// The sum of n floats (fixed order) or their maximum, over a workgroup.  The same
+// value whatever its size: lane t of a wave takes every 64th, all waves alike.
 template <bool MAX>
-__device__ __forceinline__ float wg_reduce(const float* p, int n, float* s4) {
+__device__ __forceinline__ float wave_reduce(const float* p, int n) {
     float v = 0.0f;
-    for (int i = (int)threadIdx.x; i < n; i += WG) v = MAX ? fmaxf(v, p[i]) : v + p[i];
+#pragma unroll 8
+    for (int i = lane_id(); i < n; i += 64) v = MAX ? fmaxf(v, p[i]) : v + p[i];
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) {
         const float w = __shfl_xor(v, o, 64);
         v = MAX ? fmaxf(v, w) : v + w;
     }
-    __syncthreads();
-    if (lane_id() == 0) s4[threadIdx.x >> 6] = v;
-    __syncthreads();
-    return MAX ? fmaxf(fmaxf(s4[0], s4[1]), fmaxf(s4[2], s4[3])) : (s4[0] + s4[1]) + (s4[2] + s4[3]);
+    return v;
 }
 
-// The power of two that brings the largest value to [2^13, 2^14).
-__device__ __forceinline__ int scale_of(const OMat& q, const char* ws, float* s4) {
-    const float m = wg_reduce<true>((const float*)ws, amax_wgs(q), s4);
+// The power of two that brings the largest value to [2^13, 2^14).  An fp16 update
+// is taken as it is: its squares and their sums keep
+// within fp32, and MFMA reads fp16 subnormals.
+__device__ __forceinline__ int scale_of(const OMat& q, const char* ws) {
+    if (!q.scaled) return 0;
+    const float m = wave_reduce<true>((const float*)ws, amax_wgs(q));
     int e = 0;
     if (m > 0.0f && m < INFINITY) frexpf(m, &e);
     return max(-126, min(126, m > 0.0f ? 14 - e : 0));
 }
 
 // 1 / (|G| + eps) for X as it is stored: 0 for zeros, NaN where |G| is not finite.
-__device__ __forceinline__ float norm_factor(const OMat& q, const char* ws, float eps, float* s4) {
-    const int e = scale_of(q, ws, s4);
-    const float t = wg_reduce<false>((const float*)(ws + W_SUM), prep_wgs(q), s4);
+__device__ __forceinline__ float norm_factor(const OMat& q, const char* ws, float eps) {
+    const int e = scale_of(q, ws);
+    const float t = wave_reduce<false>((const float*)(ws + W_SUM), prep_wgs(q));
     return t == 0.0f ? 0.0f : t < INFINITY ? 1.0f / (sqrtf(t) + ldexpf(eps, e)) : NAN;
 }
 
 // X [sp][Lp] and its transpose [Lp][sp] from the update, and its squares.
 template <typename T>
 __global__ __launch_bounds__(WG) void k_orth_prep(Table tb) {
-    constexpr int NP = sizeof(T) == 4 ? 2 : 1;
+    constexpr int NP = sizeof(T) == 4 ? 2 : 1, V = 16 / (int)sizeof(T);
     __shared__ float C[64 * CP<64>];
     __shared__ float s4[WG / 64];
-    const Place p = place(tb, [](const OMat& q) { return prep_wgs(q); });
+    const Place p = place(tb, [](const OMat& q) { return prep_wgs(q); }, (int)blockIdx.x);
     const OMat& q = tb.mat[p.mat];
     const T* g = (const T*)q.g + p.b * q.bstride;
     char* ws = q.ws + p.b * q.ws_one;
-    const int e = scale_of(q, ws, s4), tid = (int)threadIdx.x;
+    const int e = scale_of(q, ws), tid = (int)threadIdx.x;
     const bool tall = q.m > q.n;
     const int mp = tall ? q.Lp : q.sp, np = tall ? q.sp : q.Lp, tn = np / 64, tiles = (mp / 64) * tn, wgs = prep_wgs(q);
     char* X = ws + W_X;                     // [sp][Lp]
@@ -199,16 +233,36 @@ __global__ __launch_bounds__(WG) void k_orth_prep(Table tb) {
     float sum = 0.0f;
     for (int t = p.t; t < tiles; t += wgs) {
         const int r0 = t / tn * 64, c0 = t % tn * 64;
+        if (q.vec & 1) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int r = r0 + i * 4 + (tid >> 6), c = c0 + (tid & 63);
-            const float v = r < q.m && c < q.n ? ldexpf(to_f32(g[r * q.ld + c]), e) : 0.0f;
-            C[(i * 4 + (tid >> 6)) * CP<64> + (tid & 63)] = v;
-            sum += v * v;
+            for (int i = 0; i < 64 * 64 / V / WG; ++i) {
+                const int x = i * WG + tid, r = x / (64 / V), c = x % (64 / V) * V;
+                Vec<T, V> in;
+                in.raw = uint4{0u, 0u, 0u, 0u};
+                const T* row = g + (r0 + r) * q.ld + c0;
+                if (r0 + r < q.m && c0 + c + V <= q.n) in.raw = *reinterpret_cast<const uint4*>(row + c);
+                else if (r0 + r < q.m)
+                    for (int k = 0; k < V; ++k)
+                        if (c0 + c + k < q.n) in.e[k] = row[c + k];
+#pragma unroll
+                for (int k = 0; k < V; ++k) {
+                    const float v = ldexpf(to_f32(in.e[k]), e);
+                    C[r * CP<64> + c + k] = v;
+                    sum += v * v;
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int r = i * 4 + (tid >> 6), c = tid & 63;
+                const float v = r0 + r < q.m && c0 + c < q.n ? ldexpf(to_f32(g[(r0 + r) * q.ld + c0 + c]), e) : 0.0f;
+                C[r * CP<64> + c] = v;
+                sum += v * v;
+            }
         }
         __syncthreads();
-        store_tile<64, NP>(C, tall ? Xt : X, np, r0, c0, false);
-        store_tile<64, NP>(C, tall ? X : Xt, mp, c0, r0, true);
+        store_tile<64, NP, false, 64, WG>(C, tall ? Xt : X, np, r0, c0);
+        store_tile<64, NP, true, 64, WG>(C, tall ? X : Xt, mp, c0, r0);
         __syncthreads();
     }
 #pragma unroll
@@ -220,97 +274,159 @@ __global__ __launch_bounds__(WG) void k_orth_prep(Table tb) {
 
 // ---------------------------------------------------------------------------
 // A T x T tile of A B^T, K in steps of 32: both operands' rows go to LDS by DMA
-// (16 bytes a lane) while the step before is multiplied.  128 (64) bytes a row
-// and step, its 16-byte chunks XORed by the row, so that the rows which an MFMA
-// operand reads together lie in distinct banks.  Four waves, each a quarter of
+// (16 bytes a lane) while the steps before are multiplied.  128 (64) bytes a row
+// and step, its 16-byte chunks XORed by the pair (four) of rows, so that 16 rows
+// lie in distinct ones of the 64 banks (XORed by the row, with 8 distinct, a read
+// took twice the cycles).  Four waves, each a quarter of
 // the tile in v_mfma_f32_32x32x16_f16.
 // ---------------------------------------------------------------------------
 template <int T> constexpr int MF = T / 64;  // 32 x 32 fragments of a wave, each way
 
 template <int NP>
 __device__ __forceinline__ int chunk_of(int row, int c) {  // where chunk c of a row lies
-    return NP == 2 ? c ^ (row & 7) : c ^ ((row >> 1) & 3);
+    return NP == 2 ? c ^ ((row >> 1) & 7) : c ^ ((row >> 2) & 3);
 }
 
-template <int T, int NP>
-__device__ __forceinline__ void stage(const char* rows, long long pitch, int step, unsigned char* lds) {
-    const int tid = (int)threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-#pragma unroll
-    for (int i = 0; i < T * 4 * NP / WG; ++i) {
-        const int c = i * WG + tid, r = c / (4 * NP);
-        const char* src = rows + r * pitch + (long long)step * (64 * NP) + chunk_of<NP>(r, c % (4 * NP)) * 16;
-        __builtin_amdgcn_global_load_lds(src, (lds_ptr)(lds + (i * WG + wave * 64) * 16), 16, 0, 0);
-    }
+// Steps of 32 that a stage holds, and the elements of K of one: with tiles of 64 the
+// latency of a stage (LDS reads, then the chain of MFMAs) counts, so it is longer.
+template <int T> constexpr int KS = T == 64 ? 2 : 1;
+template <int T> constexpr __host__ __device__ int step_k() { return 32 * KS<T>; }
+template <int T, int NA, int NB> constexpr int stage_bytes() { return T * 64 * KS<T> * (NA + NB); }
+// Stages in LDS.  Tiles of 128: as many as leave room for two workgroups on a CU.
+// Tiles of 64 are for products that do not fill the chip: one workgroup a CU,
+// and what it has in flight against the latency of another XCD's results decides.
+template <int T, int NA, int NB> constexpr int stages() {
+    return T == 128 ? std::max(2, 66 * 1024 / stage_bytes<T, NA, NB>()) : 4;
 }
-
-template <int T, int NA, int NB> constexpr int stage_bytes() { return T * 64 * (NA + NB); }
 template <int T, int NA, int NB> constexpr int product_lds() {
-    return std::max(2 * stage_bytes<T, NA, NB>(), T * CP<T> * 4);
+    return std::max(stages<T, NA, NB>() * stage_bytes<T, NA, NB>(), T * CP<T> * 4);
 }
 
-__device__ __forceinline__ void product_barrier() {  // the DMA before it has landed, for all waves
-    __builtin_amdgcn_s_waitcnt(0);
+// All waves' DMA but the last `left` instructions of each has landed, and their
+// reads of the stage before are done.
+template <int LEFT>
+__device__ __forceinline__ void product_barrier() {
+    static_assert(LEFT < 64, "vmcnt");
+    __builtin_amdgcn_s_waitcnt((LEFT & 15) | 7 << 4 | (LEFT >> 4) << 14);
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 }
 
+__device__ __forceinline__ floatx16 mfma(halfx8 a, halfx8 b, floatx16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+
+// 16 bytes a lane to the wave's 1 KB at `to`.
+__device__ __forceinline__ void dma16(const char* from, unsigned char* to) {
+    __builtin_amdgcn_global_load_lds(from, (lds_ptr)to, 16, 0, 0);
+}
+
 // rows of A and B from their first element on; the tile ends in LDS as fp32.
+//
+// A wave's DMA instructions are spread over its MFMAs: a CU takes one (1 KB) in
+// about 28 cycles, and a wave that issues a stage's eight in a row stands still
+// until the last is taken (4096^2 x 4096: loads alone 100 us, MFMAs alone 112, one
+// after the other 207).
 template <int T, int NA, int NB>
 __device__ __forceinline__ void product_tile(const char* A, long long pa, const char* B, long long pb, int step0,
                                              int steps, unsigned char* lds) {
-    constexpr int SB = stage_bytes<T, NA, NB>(), OB = T * 64 * NA;
-    const int l = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    constexpr int SB = stage_bytes<T, NA, NB>(), HB = T * 64 * (NA + NB), OB = T * 64 * NA, NST = stages<T, NA, NB>();
+    // DMA instructions of a group of four waves and step of 32; of a wave and stage
+    constexpr int LA = T * 4 * NA / WG, LB = T * 4 * NB / WG, LH = LA + LB, GROUPS = NT<T> / WG;
+    constexpr int LOADS = KS<T> * LH / GROUPS;
+    static_assert(KS<T> % GROUPS == 0, "a group takes whole steps of 32");
+    // the three products of a 64 x 64 tile's one fragment in sums of their own:
+    // an MFMA waits for the one before it on the same sum
+    constexpr int CH = T == 64 ? NA + NB - 1 : 1;
+    const int tid = (int)threadIdx.x & (WG - 1), l = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int group = GROUPS == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x / WG);
     const int ra = (wave >> 1) * (T / 2) + (l & 31), rb = (wave & 1) * (T / 2) + (l & 31);
-    floatx16 acc[MF<T>][MF<T>] = {};
-    stage<T, NA>(A, pa, step0, lds);
-    stage<T, NB>(B, pb, step0, lds + OB);
-    for (int s = 0; s < steps; ++s) {
-        product_barrier();
-        unsigned char* cur = lds + (s & 1) * SB;
-        if (s + 1 < steps) {
-            unsigned char* nxt = lds + (~s & 1) * SB;
-            stage<T, NA>(A, pa, step0 + s + 1, nxt);
-            stage<T, NB>(B, pb, step0 + s + 1, nxt + OB);
-        }
+    // this lane's 16 bytes of every instruction, from the operand's first row
+    unsigned from[LH];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int c = 2 * j + (l >> 5);
-            halfx8 fa[NA][MF<T>], fb[NB][MF<T>];
+    for (int i = 0; i < LH; ++i) {
+        const int np = i < LA ? NA : NB, c = (i < LA ? i : i - LA) * WG + tid, r = c / (4 * np);
+        const int chunk = i < LA ? chunk_of<NA>(r, c % (4 * NA)) : chunk_of<NB>(r, c % (4 * NB));
+        from[i] = (unsigned)(r * (i < LA ? pa : pb) + chunk * 16);
+    }
+    auto dma = [&](int i, int s, int buf) {  // instruction i of stage s
+        const int k = i / LH * GROUPS + group, j = i % LH, np = j < LA ? NA : NB;
+        const char* base = (j < LA ? A : B) + ((long long)(step0 + s) * KS<T> + k) * (64 * np);
+        unsigned char* to = lds + buf * SB + k * HB + (j < LA ? j : j - LA) * (WG * 16) + (j < LA ? 0 : OB) + wave * 1024;
+        dma16(base + from[j], to);
+    };
+    floatx16 acc[CH][MF<T>][MF<T>] = {};
+    for (int s = 0; s < min(NST - 1, steps); ++s)
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) dma(i, s, s);
+    int at = 0;
+    for (int s = 0; s < steps; ++s) {
+        if (s + NST - 2 < steps) product_barrier<(NST - 2) * LOADS>();
+        else product_barrier<0>();
+        const unsigned char* cur = lds + at * SB;
+        const bool more = s + NST - 1 < steps;
+        const int into = at == 0 ? NST - 1 : at - 1;
+        at = at + 1 == NST ? 0 : at + 1;
+        constexpr int J = 2 * KS<T> / GROUPS;
+        halfx8 fa[J][NA][MF<T>], fb[J][NB][MF<T>];  // of the whole stage: their reads are in flight together
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const int c = 2 * (j & 1) + (l >> 5);
+            const unsigned char* half = cur + ((j >> 1) * GROUPS + group) * HB;
 #pragma unroll
             for (int i = 0; i < MF<T>; ++i) {
 #pragma unroll
                 for (int h = 0; h < NA; ++h)
-                    fa[h][i] = *(const halfx8*)(cur + (ra + 32 * i) * (64 * NA) + chunk_of<NA>(ra + 32 * i, 4 * h + c) * 16);
+                    fa[j][h][i] = *(const halfx8*)(half + (ra + 32 * i) * (64 * NA) + chunk_of<NA>(ra + 32 * i, 4 * h + c) * 16);
 #pragma unroll
                 for (int h = 0; h < NB; ++h)
-                    fb[h][i] = *(const halfx8*)(cur + OB + (rb + 32 * i) * (64 * NB) +
-                                                chunk_of<NB>(rb + 32 * i, 4 * h + c) * 16);
+                    fb[j][h][i] = *(const halfx8*)(half + OB + (rb + 32 * i) * (64 * NB) +
+                                                   chunk_of<NB>(rb + 32 * i, 4 * h + c) * 16);
             }
+        }
+        constexpr int MM = J * (NA + NB - 1) * MF<T> * MF<T>;  // MFMAs of a stage
+        int m = 0, d = 0;
 #pragma unroll
-            for (int h = 0; h < NA + NB - 1; ++h)  // hi hi, hi lo, lo hi
+        for (int j = 0; j < J; ++j)
+#pragma unroll
+            for (int h = 0; h < NA + NB - 1; ++h) {  // hi hi, hi lo, lo hi
+                constexpr int LO_A = NB == 2 ? 2 : 1;
+                const int ha = NA == 2 && h == LO_A ? 1 : 0, hb = NB == 2 && h == 1 ? 1 : 0;
 #pragma unroll
                 for (int x = 0; x < MF<T>; ++x)
 #pragma unroll
                     for (int y = 0; y < MF<T>; ++y) {
-                        const int ha = h == (NB == 2 ? 2 : 1) ? 1 : 0, hb = NB == 2 && h == 1 ? 1 : 0;
-                        acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa[ha < NA ? ha : 0][x], fb[hb < NB ? hb : 0][y],
-                                                                           acc[x][y], 0, 0, 0);
+                        acc[h % CH][x][y] = mfma(fa[j][ha][x], fb[j][hb][y], acc[h % CH][x][y]);
+                        ++m;
+                        while (d * MM < m * LOADS) {
+                            __builtin_amdgcn_sched_barrier(0);
+                            if (more) dma(d, s + NST - 1, into);
+                            __builtin_amdgcn_sched_barrier(0);
+                            ++d;
+                        }
                     }
-        }
+            }
     }
-    __syncthreads();
+#pragma unroll
+    for (int h = 1; h < CH; ++h) acc[0][0][0] += acc[h][0][0];
     float* C = (float*)lds;
 #pragma unroll
-    for (int x = 0; x < MF<T>; ++x)
+    for (int g = GROUPS - 1; g >= 0; --g) {  // the last group's sums, then the first's on top
+        __syncthreads();
+        if (g == group)
 #pragma unroll
-        for (int y = 0; y < MF<T>; ++y)
+            for (int x = 0; x < MF<T>; ++x)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int i = (wave >> 1) * (T / 2) + 32 * x + (r & 3) + 8 * (r >> 2) + 4 * (l >> 5);
-                const int j = (wave & 1) * (T / 2) + 32 * y + (l & 31);
-                C[i * CP<T> + j] = acc[x][y][r];
-            }
+                for (int y = 0; y < MF<T>; ++y)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int i = (wave >> 1) * (T / 2) + 32 * x + (r & 3) + 8 * (r >> 2) + 4 * (l >> 5);
+                        const int j = (wave & 1) * (T / 2) + 32 * y + (l & 31);
+                        float& c = C[i * CP<T> + j];
+                        c = g == GROUPS - 1 ? acc[0][x][y][r] : c + acc[0][x][y][r];
+                    }
+    }
     __syncthreads();
 }
 
@@ -319,20 +435,38 @@ __device__ __forceinline__ int sym_tiles(const OMat& q) {
     const int t = q.sp / T;
     return t * (t + 1) / 2;
 }
-__device__ __forceinline__ void sym_tile(int t, int& bi, int& bj) {  // the t-th tile with bi >= bj
-    bi = (int)((sqrtf(8.0f * t + 1.0f) - 1.0f) * 0.5f);
-    while ((bi + 1) * (bi + 2) / 2 <= t) ++bi;
-    while (bi * (bi + 1) / 2 > t) --bi;
-    bj = t - bi * (bi + 1) / 2;
+__device__ __forceinline__ void triangle(int t, int& i, int& j) {  // the t-th of (0, 0), (1, 0), (1, 1), ...
+    i = (int)((sqrtf(8.0f * t + 1.0f) - 1.0f) * 0.5f);
+    while ((i + 1) * (i + 2) / 2 <= t) ++i;
+    while (i * (i + 1) / 2 > t) --i;
+    j = t - i * (i + 1) / 2;
+}
+// The t-th tile with bi >= bj of n x n: strips of eight rows of tiles, each column
+// by column, so that 64 neighbours (what an XCD works on at a time) read 16
+// panels and not 35.
+__device__ __forceinline__ void sym_tile(int t, int n, int& bi, int& bj) {
+    int S = (int)((sqrtf(16.0f + 128.0f * t) - 4.0f) * (1.0f / 64.0f));  // 32 S^2 + 4 S tiles before strip S
+    while (32 * (S + 1) * (S + 1) + 4 * (S + 1) <= t) ++S;
+    while (32 * S * S + 4 * S > t) --S;
+    const int local = t - 32 * S * S - 4 * S, h = min(8, n - 8 * S), square = 8 * S * h;
+    if (local < square) {
+        bj = local / h;
+        bi = 8 * S + (local - bj * h);
+    } else {
+        triangle(local - square, bi, bj);
+        bi += 8 * S;
+        bj += 8 * S;
+    }
 }
 
-// out = alpha C + beta D + gamma I, out and D symmetric [sp][sp], the tile and its mirror image.
-template <int T>
-__device__ __forceinline__ void store_sym(float* C, char* out, const char* D, int sp, int bi, int bj, float alpha,
-                                          float beta, float gamma) {
-    for (int e = (int)threadIdx.x; e < T * T / 8; e += WG) {
-        const int r = e / (T / 8), k = (e % (T / 8)) * 8, R = bi * T + r, K = bj * T + k;
-        const long long row = (long long)R * sp * 4;
+// out = alpha C + beta D + gamma I for R x T cells at (r0, c0) of symmetric
+// matrices [sp][sp], and their mirror image.
+template <int T, int R>
+__device__ __forceinline__ void store_sym(float* C, char* out, const char* D, int sp, int r0, int c0, bool mirror,
+                                          float alpha, float beta, float gamma) {
+    for (int e = (int)threadIdx.x; e < R * T / 8; e += NT<T>) {
+        const int r = e / (T / 8), k = (e % (T / 8)) * 8, K = c0 + k;
+        const long long row = (long long)(r0 + r) * sp * 4;
         float v[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = alpha * C[r * CP<T> + k + i];
@@ -340,114 +474,306 @@ __device__ __forceinline__ void store_sym(float* C, char* out, const char* D, in
             const Vec<f16, 8> hi = vload<f16, 8>((const f16*)(D + row + at_k<2>(K)));
             const Vec<f16, 8> lo = vload<f16, 8>((const f16*)(D + row + at_k<2>(K) + 64));
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] += beta * ((float)hi.e[i] + (float)lo.e[i]) + (R == K + i ? gamma : 0.0f);
+            for (int i = 0; i < 8; ++i)
+                v[i] += beta * ((float)hi.e[i] + (float)lo.e[i]) + (r0 + r == K + i ? gamma : 0.0f);
         }
         store8<2>(out + row, K, v);
 #pragma unroll
         for (int i = 0; i < 8; ++i) C[r * CP<T> + k + i] = v[i];
     }
-    if (bi == bj) return;
+    if (!mirror) return;
     __syncthreads();
-    store_tile<T, 2>(C, out, sp, bj * T, bi * T, true);
+    store_tile<T, 2, true, R>(C, out, sp, c0, r0);
 }
 
-// A <- X X^T (times norm_factor^2 in the first block) or its parts over K.
-template <int T, int NP>
-__global__ __launch_bounds__(WG, 2) void k_orth_gram(Table tb, float alpha, float eps, int first) {
-    extern __shared__ __align__(16) unsigned char lds[];
-    __shared__ float s4[WG / 64];
-    // (tile, part): the parts of a tile are neighbours
-    const Place p = place(tb, [](const OMat& q) { return sym_tiles<T>(q) * q.splits; });
-    const OMat& q = tb.mat[p.mat];
-    char* ws = q.ws + p.b * q.ws_one;
-    int bi, bj;
-    sym_tile(p.t / q.splits, bi, bj);
-    const int part = p.t % q.splits, all = q.Lp / 32, k0 = (int)((long long)all * part / q.splits),
-              k1 = (int)((long long)all * (part + 1) / q.splits);
-    const long long pitch = (long long)q.Lp * (2 * NP);
-    const char* X = ws + W_X;
-    product_tile<T, NP, NP>(X + bi * T * pitch, pitch, X + bj * T * pitch, pitch, k0, k1 - k0, lds);
-    float* C = (float*)lds;
-    if (q.splits > 1) {
-        float* out = (float*)(ws + w_sym(q.sp, q.Lp, SYMS)) + (long long)p.t * (T * T);
-        for (int e = (int)threadIdx.x; e < T * T; e += WG) out[e] = C[e / T * CP<T> + e % T];
-        return;
-    }
-    const float f = first ? norm_factor(q, ws, eps, s4) : 1.0f;
-    store_sym<T>(C, ws + w_sym(q.sp, q.Lp, 0), nullptr, q.sp, bi, bj, alpha * f * f, 0.0f, 0.0f);
-}
-
-// The parts added in their order.
-template <int T>
-__global__ __launch_bounds__(WG) void k_orth_parts(Table tb, float alpha, float eps, int first) {
-    extern __shared__ __align__(16) unsigned char lds[];
-    __shared__ float s4[WG / 64];
-    const Place p = place(tb, [](const OMat& q) { return q.splits > 1 ? sym_tiles<T>(q) : 0; });
-    const OMat& q = tb.mat[p.mat];
-    char* ws = q.ws + p.b * q.ws_one;
-    int bi, bj;
-    sym_tile(p.t, bi, bj);
-    const float* in = (const float*)(ws + w_sym(q.sp, q.Lp, SYMS)) + (long long)p.t * q.splits * (T * T);
-    float* C = (float*)lds;
-    for (int e = (int)threadIdx.x; e < T * T; e += WG) {
-        float v = in[e];
-        for (int k = 1; k < q.splits; ++k) v += in[(long long)k * (T * T) + e];
-        C[e / T * CP<T> + e % T] = v;
-    }
-    const float f = first ? norm_factor(q, ws, eps, s4) : 1.0f;
-    __syncthreads();
-    store_sym<T>(C, ws + w_sym(q.sp, q.Lp, 0), nullptr, q.sp, bi, bj, alpha * f * f, 0.0f, 0.0f);
-}
-
-// One or two products of symmetric matrices (numbers of the workspace's):
-// c = alpha a b + beta d + gamma I.
+// One or two products that give symmetric matrices (numbers of the
+// workspace's): c = alpha a b + beta d + gamma I, or c = alpha f^2 X X^T with f the
+// norm's factor in the first block.  A tile is a workgroup's, or it is split over
+// K among several (units) that leave their sums for k_orth_join:
+//   whole >= 0: the tiles of the entries, of the first product and then of the
+//     second, are numbered through; those from `whole` on have `parts` units each;
+//   whole < 0 (X X^T alone): every entry's tiles have `parts` of its own.
 struct SymJob {
     int a, b, c, d;
     float alpha, beta, gamma;
 };
+struct SymLaunch {
+    SymJob job[2];
+    int tiles;  // of one product
+    int whole, parts, first;
+    int leave;  // sums of every tile, for k_orth_steps
+    float eps;
+    float* sums;  // [unit][T * T], units counted from the first split tile's (whole < 0: from the first of all)
+};
+
+struct SymUnit {
+    Place p;
+    int job, part, parts;
+    long long unit;
+};
 template <int T>
-__global__ __launch_bounds__(WG, 2) void k_orth_sym(Table tb, SymJob j0, SymJob j1) {
-    extern __shared__ __align__(16) unsigned char lds[];
-    const Place p = place(tb, [](const OMat& q) { return sym_tiles<T>(q); });
-    const OMat& q = tb.mat[p.mat];
-    const SymJob& j = blockIdx.y ? j1 : j0;
-    char* ws = q.ws + p.b * q.ws_one;
+__device__ __forceinline__ SymUnit sym_unit(const Table& tb, const SymLaunch& s, int bid) {
+    auto tiles = [](const OMat& q) { return sym_tiles<T>(q); };
+    if (s.whole < 0) {
+        Place p = place(tb, [](const OMat& q) { return sym_tiles<T>(q) * q.parts; }, bid);
+        const OMat& q = tb.mat[p.mat];
+        const int u = p.t, n = sym_tiles<T>(q);
+        p.t = u / q.parts;
+        return SymUnit{p, 0, u % q.parts, q.parts, q.unit0 + ((long long)p.b * n + p.t) * q.parts + u % q.parts};
+    }
+    const int over = bid - s.whole, tile = over < 0 ? bid : s.whole + over / s.parts, job = tile >= s.tiles;
+    return SymUnit{place(tb, tiles, tile - job * s.tiles), job, over < 0 ? 0 : over % s.parts, over < 0 ? 1 : s.parts, over};
+}
+
+// C: R rows of the tile from row `part` R on.
+template <int T, int R, bool GRAM>
+__device__ __forceinline__ void sym_out(const OMat& q, char* ws, const SymLaunch& s, const SymJob& j, int t, int part,
+                                        float* C) {
     int bi, bj;
-    sym_tile(p.t, bi, bj);
-    const long long pitch = (long long)q.sp * 4;
+    sym_tile(t, q.sp / T, bi, bj);
     auto sym = [&](int i) { return ws + w_sym(q.sp, q.Lp, i); };
-    product_tile<T, 2, 2>(sym(j.a) + bi * T * pitch, pitch, sym(j.b) + bj * T * pitch, pitch, 0, q.sp / 32, lds);
-    store_sym<T>((float*)lds, sym(j.c), j.d < 0 ? nullptr : sym(j.d), q.sp, bi, bj, j.alpha, j.beta, j.gamma);
+    float alpha = j.alpha;
+    if (GRAM && s.first) {
+        const float f = norm_factor(q, ws, s.eps);
+        alpha *= f * f;
+    }
+    store_sym<T, R>(C, sym(j.c), GRAM || j.d < 0 ? nullptr : sym(j.d), q.sp, bi * T + part * R, bj * T, bi != bj, alpha,
+                    j.beta, j.gamma);
+}
+
+template <int T, int NP, bool GRAM>
+__global__ __launch_bounds__(NT<T>, 2) void k_orth_sym(Table tb, SymLaunch s) {
+    extern __shared__ __align__(16) unsigned char lds[];
+    const SymUnit u = sym_unit<T>(tb, s, (int)blockIdx.x);
+    const OMat& q = tb.mat[u.p.mat];
+    const SymJob& j = s.job[u.job];
+    char* ws = q.ws + u.p.b * q.ws_one;
+    int bi, bj;
+    sym_tile(u.p.t, q.sp / T, bi, bj);
+    const int K = GRAM ? q.Lp : q.sp, steps = K / step_k<T>();
+    const int k0 = (int)((long long)steps * u.part / u.parts), k1 = (int)((long long)steps * (u.part + 1) / u.parts);
+    const long long pitch = (long long)K * (2 * NP);
+    const char* A = GRAM ? ws + W_X : ws + w_sym(q.sp, q.Lp, j.a);
+    const char* B = GRAM ? A : ws + w_sym(q.sp, q.Lp, j.b);
+    product_tile<T, NP, NP>(A + bi * T * pitch, pitch, B + bj * T * pitch, pitch, k0, k1 - k0, lds);
+    float* C = (float*)lds;
+    if (u.parts > 1 || s.leave) {
+        float4* out = (float4*)(s.sums + u.unit * (T * T));
+        for (int e = (int)threadIdx.x; e < T * T / 4; e += NT<T>) {
+            const float* c = C + e / (T / 4) * CP<T> + e % (T / 4) * 4;
+            out[e] = float4{c[0], c[1], c[2], c[3]};
+        }
+        return;
+    }
+    sym_out<T, T, GRAM>(q, ws, s, j, u.p.t, 0, C);
+}
+
+// The parts of the split tiles added in their order, a few rows a workgroup.
+template <int T> constexpr int JOIN_ROWS = T == 64 ? 32 : 16;
+template <int T, bool GRAM>
+__global__ __launch_bounds__(NT<T>) void k_orth_join(Table tb, SymLaunch s) {
+    constexpr int R = JOIN_ROWS<T>, N = R * T / 4 / NT<T>;  // vectors of a thread
+    __shared__ float C[R * CP<T>];
+    SymUnit u;
+    int slice;
+    if (s.whole < 0) {  // (the launch is numbered by slices of the tiles with several parts)
+        u.p = place(tb, [](const OMat& q) { return q.parts > 1 ? sym_tiles<T>(q) * (T / R) : 0; }, (int)blockIdx.x);
+        const OMat& q = tb.mat[u.p.mat];
+        slice = u.p.t % (T / R);
+        u.p.t /= T / R;
+        u.job = 0;
+        u.parts = q.parts;
+        u.unit = q.unit0 + ((long long)u.p.b * sym_tiles<T>(q) + u.p.t) * q.parts;
+    } else {
+        slice = (int)blockIdx.x % (T / R);
+        u = sym_unit<T>(tb, s, s.whole + (int)blockIdx.x / (T / R) * s.parts);
+    }
+    const OMat& q = tb.mat[u.p.mat];
+    const float4* in = (const float4*)(s.sums + u.unit * (T * T) + slice * (R * T));
+    float4 sum[N] = {};
+#pragma unroll 4
+    for (int k = 0; k < u.parts; ++k)
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float4 v = in[(long long)k * (T * T / 4) + i * NT<T> + (int)threadIdx.x];
+            sum[i] = float4{sum[i].x + v.x, sum[i].y + v.y, sum[i].z + v.z, sum[i].w + v.w};
+        }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int e = i * NT<T> + (int)threadIdx.x;
+        float* c = C + e / (T / 4) * CP<T> + e % (T / 4) * 4;
+        c[0] = sum[i].x;
+        c[1] = sum[i].y;
+        c[2] = sum[i].z;
+        c[3] = sum[i].w;
+    }
+    __syncthreads();
+    sym_out<T, R, GRAM>(q, q.ws + u.p.b * q.ws_one, s, s.job[u.job], u.p.t, slice, C);
+}
+
+// A block of steps on matrices of one tile (s <= 64) without leaving a workgroup:
+// from the sums of X X^T to Q, everything in LDS.  As launches of their own its
+// products took 4.6 us each, whatever they compute (a filter of 64 x 576, 13
+// products: 60 us; here the whole block takes 7.4 to 11 us).  Four waves a product, the eight share T and Q.
+struct Steps {
+    int len, first, Q;  // Q: where it goes
+    float a0, eps;      // A = a0 f^2 X X^T
+    const float* sums;
+    struct One {
+        float aa, a, i, t, n, q;  // P = aa A A + a A + i I,  T = t P A,  A = n T P,  Q = q P Q
+    } one[8];  // (blocks are no longer)
+};
+constexpr int STEP_MAX = 8;
+constexpr int STEPS_LDS = 5 * 64 * 256;
+
+// Where 8 elements k.. of a row lie in a matrix in LDS (the hi part; lo is chunk + 4).
+__device__ __forceinline__ int step_at(int row, int k, bool lo) {
+    return (k >> 5) * (64 * 128) + row * 128 + chunk_of<2>(row, (k >> 3 & 3) + (lo ? 4 : 0)) * 16;
+}
+
+// c = alpha (a b^T)^T + beta d + gamma I by four waves (d nullptr: the product
+// alone).  All of them are symmetric up to rounding, and the product is stored
+// transposed, four elements a lane.  The order of the factors counts: with
+// T = P A^T (a = A, b = P) the next A = P T^T = P A P^T is a congruence, which keeps
+// it symmetric; as P P A^T the little by which P and A do not commute grows as
+// an error of A does (bf16, 64 x 64: 8e-3 off and not 1.7e-3).
+__device__ __forceinline__ void step_product(const unsigned char* a, const unsigned char* b, unsigned char* c,
+                                             const unsigned char* d, float alpha, float beta, float gamma) {
+    const int l = lane_id(), wave = (int)threadIdx.x >> 6 & 3;
+    const int ra = (wave >> 1) * 32 + (l & 31), rb = (wave & 1) * 32 + (l & 31);
+    halfx8 fa[4][2], fb[4][2];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int k = 16 * j + 8 * (l >> 5);
+            fa[j][h] = *(const halfx8*)(a + step_at(ra, k, h));
+            fb[j][h] = *(const halfx8*)(b + step_at(rb, k, h));
+        }
+    floatx16 acc[3] = {};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        acc[0] = mfma(fa[j][0], fb[j][0], acc[0]);
+        acc[1] = mfma(fa[j][0], fb[j][1], acc[1]);
+        acc[2] = mfma(fa[j][1], fb[j][0], acc[2]);
+    }
+    acc[0] += acc[1] + acc[2];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const int k = (wave >> 1) * 32 + 8 * q + 4 * (l >> 5), at = (k & 4) * 2;  // this lane's rows k..k+3 of column rb
+        unsigned char* hi = c + step_at(rb, k & ~7, false) + at;
+        unsigned char* lo = c + step_at(rb, k & ~7, true) + at;
+        Vec<f16, 4> dh, dl, h, g;
+        if (d) {
+            dh = vload<f16, 4>((const f16*)(d + (hi - c)));
+            dl = vload<f16, 4>((const f16*)(d + (lo - c)));
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float v = alpha * acc[0][4 * q + i];
+            if (d) v += beta * ((float)dh.e[i] + (float)dl.e[i]) + (rb == k + i ? gamma : 0.0f);
+            asm("" : "+v"(v));  // (see store8)
+            h.e[i] = (f16)v;
+            g.e[i] = (f16)(v - (float)h.e[i]);
+        }
+        vstore<f16, 4>((f16*)hi, h);
+        vstore<f16, 4>((f16*)lo, g);
+    }
+}
+
+__global__ __launch_bounds__(512) void k_orth_steps(Table tb, Steps st) {
+    extern __shared__ __align__(16) unsigned char lds[];
+    const Place p = place(tb, [](const OMat&) { return 1; }, (int)blockIdx.x);
+    const OMat& q = tb.mat[p.mat];
+    char* ws = q.ws + p.b * q.ws_one;
+    const int tid = (int)threadIdx.x, group = __builtin_amdgcn_readfirstlane(tid >> 8);
+    auto sym = [&](int i) { return lds + i * (64 * 256); };
+    const float f = st.first ? norm_factor(q, ws, st.eps) : 1.0f;
+    {
+        const int row = tid >> 3, k = (tid & 7) * 8;
+        const float* in = st.sums + (q.unit0 + (long long)p.b * q.parts) * 4096 + row * 64 + k;
+        float v[8] = {};
+#pragma unroll 4
+        for (int n = 0; n < q.parts; ++n) {
+            const float4 x = *(const float4*)(in + n * 4096LL), y = *(const float4*)(in + n * 4096LL + 4);
+            const float w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] += w[i];
+        }
+        Vec<f16, 8> hi, lo;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            float x = v[i] * (st.a0 * f * f);
+            asm("" : "+v"(x));  // (see store8)
+            hi.e[i] = (f16)x;
+            lo.e[i] = (f16)(x - (float)hi.e[i]);
+        }
+        vstore<f16, 8>((f16*)(sym(0) + step_at(row, k, false)), hi);
+        vstore<f16, 8>((f16*)(sym(0) + step_at(row, k, true)), lo);
+    }
+    int Q = -1;
+    for (int n = 0; n < st.len; ++n) {
+        const Steps::One& o = st.one[n];
+        const int P = Q == 2 ? 3 : 2, Q2 = Q < 0 ? P : 9 - Q - P;
+        const bool more = n + 1 < st.len;
+        __syncthreads();
+        if (group == 0) step_product(sym(0), sym(0), sym(P), sym(0), o.aa, o.a, o.i);
+        __syncthreads();
+        if (group == 0 && more) step_product(sym(0), sym(P), sym(1), nullptr, o.t, 0.0f, 0.0f);
+        if (group == 1 && Q >= 0) step_product(sym(Q), sym(P), sym(Q2), nullptr, o.q, 0.0f, 0.0f);
+        if (more) {
+            __syncthreads();
+            if (group == 0) step_product(sym(1), sym(P), sym(0), nullptr, o.n, 0.0f, 0.0f);
+        }
+        Q = Q2;
+    }
+    __syncthreads();
+    char* out = ws + w_sym(q.sp, q.Lp, st.Q);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int e = i * 512 + tid, row = e >> 4, c = e & 15;  // 16 bytes c of the row
+        *(uint4*)(out + row * 256 + c * 16) = *(const uint4*)(sym(Q) + step_at(row, (c >> 3) * 32 + (c & 3) * 8, c & 4));
+    }
 }
 
 // Q X: the next block's X and its transpose, or the result.
 template <int T, int NP, typename TO, bool LAST>
-__global__ __launch_bounds__(WG, 2) void k_orth_apply(Table tb, int Q, int xt, float alpha, float eps, int first) {
+__global__ __launch_bounds__(NT<T>, 2) void k_orth_apply(Table tb, int Q, int xt, float alpha, float eps, int first) {
     extern __shared__ __align__(16) unsigned char lds[];
-    __shared__ float s4[WG / 64];
-    const Place p = place(tb, [](const OMat& q) { return (q.sp / T) * (q.Lp / T); });
+    const Place p = place(tb, [](const OMat& q) { return (q.sp / T) * (q.Lp / T); }, (int)blockIdx.x);
     const OMat& q = tb.mat[p.mat];
     char* ws = q.ws + p.b * q.ws_one;
-    const int ts = q.sp / T, i = p.t % ts, k = p.t / ts;  // tiles of one row of Xt are neighbours
+    // strips of eight rows of Q, each along L
+    const int strip = p.t / (8 * (q.Lp / T)), h = min(8, q.sp / T - 8 * strip), local = p.t - strip * (8 * (q.Lp / T));
+    const int k = local / h, i = 8 * strip + (local - k * h);
     const char* qm = ws + w_sym(q.sp, q.Lp, Q) + (long long)i * T * q.sp * 4;
     const char* xm = ws + w_xt(q.sp, q.Lp, xt) + (long long)k * T * q.sp * (2 * NP);
     const bool tall = LAST && q.m > q.n;  // then the tile's rows are those of Xt
-    if (tall) product_tile<T, NP, 2>(xm, (long long)q.sp * (2 * NP), qm, (long long)q.sp * 4, 0, q.sp / 32, lds);
-    else product_tile<T, 2, NP>(qm, (long long)q.sp * 4, xm, (long long)q.sp * (2 * NP), 0, q.sp / 32, lds);
+    if (tall) product_tile<T, NP, 2>(xm, (long long)q.sp * (2 * NP), qm, (long long)q.sp * 4, 0, q.sp / step_k<T>(), lds);
+    else product_tile<T, 2, NP>(qm, (long long)q.sp * 4, xm, (long long)q.sp * (2 * NP), 0, q.sp / step_k<T>(), lds);
     float* C = (float*)lds;
-    const float f = alpha * (first ? norm_factor(q, ws, eps, s4) : 1.0f);
+    const float f = alpha * (first ? norm_factor(q, ws, eps) : 1.0f);
     if constexpr (LAST) {
         TO* o = (TO*)q.o + p.b * q.bstride_o;
         const int r0 = (tall ? k : i) * T, c0 = (tall ? i : k) * T;
-        for (int e = (int)threadIdx.x; e < T * T; e += WG) {
-            const int r = r0 + e / T, c = c0 + e % T;
-            if (r < q.m && c < q.n) o[r * q.ld_o + c] = from_f32<TO>(f * C[e / T * CP<T> + e % T]);
+        constexpr int V = 16 / (int)sizeof(TO);
+        for (int e = (int)threadIdx.x; e < T * T / V; e += NT<T>) {
+            const int x = e / (T / V), y = e % (T / V) * V, r = r0 + x, c = c0 + y;
+            Vec<TO, V> v;
+#pragma unroll
+            for (int i = 0; i < V; ++i) v.e[i] = from_f32<TO>(f * C[x * CP<T> + y + i]);
+            if (r >= q.m) continue;
+            TO* to = o + r * q.ld_o + c;
+            if ((q.vec & 2) && c + V <= q.n) *reinterpret_cast<uint4*>(to) = v.raw;
+            else
+                for (int i = 0; i < V; ++i)
+                    if (c + i < q.n) to[i] = v.e[i];
         }
     } else {
-        for (int e = (int)threadIdx.x; e < T * T; e += WG) C[e / T * CP<T> + e % T] *= f;
+        for (int e = (int)threadIdx.x; e < T * T; e += NT<T>) C[e / T * CP<T> + e % T] *= f;
         __syncthreads();
-        store_tile<T, 2>(C, ws + W_X, q.Lp, i * T, k * T, false);
-        store_tile<T, 2>(C, ws + w_xt(q.sp, q.Lp, xt ^ 1), q.sp, k * T, i * T, true);
+        store_tile<T, 2, false>(C, ws + W_X, q.Lp, i * T, k * T);
+        store_tile<T, 2, true>(C, ws + w_xt(q.sp, q.Lp, xt ^ 1), q.sp, k * T, i * T);
     }
 }
 
@@ -457,61 +783,79 @@ __global__ __launch_bounds__(WG, 2) void k_orth_apply(Table tb, int Q, int xt, f
 struct Group {
     Table tb;
     int entry[OM], first[OM];  // of the list, and the first matrix of its batch
-    int tile;
-    size_t bytes;
+    size_t bytes, sums;        // of the workspace, and where the sums of split products begin
 };
 
 long long up(long long n, long long k) { return (n + k - 1) / k * k; }
+
+long long sym_count(const Table& tb, int T) {
+    long long n = 0;
+    for (int i = 0; i < tb.count; ++i) {
+        const long long t = tb.mat[i].sp / T;
+        n += t * (t + 1) / 2 * tb.mat[i].batch;
+    }
+    return n;
+}
+
+// How a launch of n tiles (of `products` products) goes to the chip's slots of
+// two workgroups a CU: rounds of whole tiles, and the rest split over K (in at
+// most so many parts) so that it fills them once more.
+struct Cut {
+    int whole, parts;
+};
+constexpr int SLOTS = 512;
+Cut cut_of(long long n, int most) {
+    const int rest = (int)(n % SLOTS);
+    const int parts = rest == 0 || n < SLOTS ? 1 : std::min(SLOTS / rest, most);
+    return parts > 1 ? Cut{(int)n - rest, parts} : Cut{(int)n, 1};
+}
+
+// Tiles of 128 where they give every CU one, else of 64 (and for single tiles).
+int tile_of(long long n128, bool fits) { return fits && n128 >= 256 ? 128 : 64; }
 
 // The list cut into groups that share their launches and, one after the other,
 // the workspace.  A group ends when its matrices alone fill the chip several
 // times over, so that a long list or batch takes no more workspace than that.
 std::vector<Group> groups_of(const OrthMat* mats, int count) {
     std::vector<Group> v;
-    auto tiles = [](int s, int T) { const long long t = (s + T - 1) / T; return t * (t + 1) / 2; };
     int i = 0, b = 0;  // the next matrix
     while (i < count) {
         Group g{};
         long long work = 0;
-        int n = 0, many[OM];
+        int& n = g.tb.count;
+        int unit = 64;  // of the padded sides: single tiles of 64, or tiles of either size
         while (i < count && n < OM && work < 2048) {
-            const int s = std::min(mats[i].m, mats[i].n), L = std::max(mats[i].m, mats[i].n);
-            const long long one = tiles(s, 128) + (up(s, 128) * up(L, 128) >> 20);
-            const int take = (int)std::min<long long>(mats[i].batch - b, std::max(1LL, (2048 - work + one - 1) / one));
-            g.first[n] = b;
-            g.entry[n] = i;
-            many[n++] = take;
-            work += one * take;
-            b += take;
-            if (b == mats[i].batch) {
-                ++i;
-                b = 0;
-            }
-        }
-        g.tile = work >= 256 ? 128 : 64;
-        long long cells = 0;
-        for (int k = 0; k < n; ++k) cells += tiles(std::min(mats[g.entry[k]].m, mats[g.entry[k]].n), g.tile) * many[k];
-        for (int k = 0; k < n; ++k) {
-            const OrthMat& q = mats[g.entry[k]];
-            OMat& o = g.tb.mat[k];
+            const OrthMat& q = mats[i];
+            OMat& o = g.tb.mat[n];
+            o.s = std::min(q.m, q.n);
+            o.L = std::max(q.m, q.n);
+            const long long t = up(o.s, 128) / 128, one = t * (t + 1) / 2 + (up(o.s, 128) * up(o.L, 128) >> 20);
+            o.batch = (int)std::min<long long>(q.batch - b, std::max(1LL, (2048 - work + one - 1) / one));
             o.ld = q.ld;
             o.ld_o = q.ld_o;
             o.bstride = q.bstride;
             o.bstride_o = q.bstride_o;
-            o.batch = many[k];
             o.m = q.m;
             o.n = q.n;
-            o.s = std::min(q.m, q.n);
-            o.L = std::max(q.m, q.n);
-            o.sp = (int)up(o.s, g.tile);
-            o.Lp = (int)up(o.L, g.tile);
-            // parts over L until there are two workgroups a CU, each of 8 steps at least
-            o.splits = (int)std::max(1LL, std::min<long long>(512 / std::max(1LL, cells), o.Lp / 256));
-            o.ws_one = up(w_sym(o.sp, o.Lp, SYMS) +
-                              (o.splits > 1 ? tiles(o.s, g.tile) * o.splits * g.tile * g.tile * 4 : 0), 256);
+            unit = o.s > 64 ? 128 : unit;
+            g.first[n] = b;
+            g.entry[n++] = i;
+            work += one * o.batch;
+            b += o.batch;
+            if (b == q.batch) {
+                ++i;
+                b = 0;
+            }
+        }
+        for (int k = 0; k < n; ++k) {
+            OMat& o = g.tb.mat[k];
+            o.sp = (int)up(o.s, unit);
+            o.Lp = (int)up(o.L, unit);
+            o.ws_one = up(w_sym(o.sp, o.Lp, SYMS), 256);
             g.bytes += (size_t)(o.ws_one * o.batch);
         }
-        g.tb.count = n;
+        g.sums = g.bytes;
+        g.bytes += (size_t)2 * SLOTS * 128 * 128 * 4;  // (X X^T: less than SLOTS tiles and SLOTS parts more)
         v.push_back(g);
     }
     return v;
@@ -561,90 +905,169 @@ int exponent(double bound) {
 }
 float pow2(int e) { return (float)ldexp(1.0, std::max(-140, std::min(120, e))); }
 
-template <typename T, int TILE>
-hipError_t orth_group(Group& g, int steps, const double* coef, double eps_, hipStream_t st) {
-    constexpr int NP = sizeof(T) == 4 ? 2 : 1;
+template <typename T>
+struct Runner {
+    static constexpr int NP = sizeof(T) == 4 ? 2 : 1;
     // (see the head of this file)
-    constexpr double MAX_GROWTH = std::is_same<T, bf16>::value ? 2.1e4 : std::is_same<T, f16>::value ? 150.0 : 12.5;
-    const float eps = (float)eps_;
-    Table& tb = g.tb;
+    static constexpr double MAX_GROWTH = std::is_same<T, bf16>::value ? 2.1e4 : std::is_same<T, f16>::value ? 150.0 : 12.5;
+    Table& tb;
+    float* sums;
+    float eps;
+    hipStream_t st;
     hipError_t err = hipSuccess;
-    auto run = [&](auto kernel, unsigned grid, unsigned grid_y, int lds, auto... args) {
-        if (err != hipSuccess || grid == 0) return;
-        if (lds && (err = ensure_dyn_lds((const void*)kernel, lds)) != hipSuccess) return;
-        hipLaunchKernelGGL(kernel, dim3(grid, grid_y), dim3(WG), lds, st, tb, args...);
-        err = hipGetLastError();
-    };
-    auto syms = [](const OMat& q) { const int t = q.sp / TILE; return t * (t + 1) / 2; };
-    run(k_orth_amax<T>, number(tb, [](const OMat& q) { return std::min<long long>(MAXA, ((long long)q.m * q.n + 16383) / 16384); }), 1, 0);
-    run(k_orth_prep<T>, number(tb, [](const OMat& q) { return std::min<long long>(MAXP, (long long)(q.sp / 64) * (q.Lp / 64)); }), 1, 0);
-    double lambda = 1.0;
-    int xt = 0, ex = 0, step = 0;  // X is stored times 2^ex (and norm_factor in the first block)
-    constexpr int lds22 = product_lds<TILE, 2, 2>();
-    for (bool first = true; step < steps; first = false) {
-        int len = 0;
-        double growth = 1.0, l = lambda;
-        while (step + len < steps) {
-            if (len && growth > MAX_GROWTH) break;
-            const Bound b = bound_of(coef + 3 * (step + len), l);
-            growth *= b.p * b.p;
-            l = b.lambda;
-            ++len;
+    bool wide = true;    // sides are multiples of 128
+    bool single = true;  // every matrix is one tile of 64
+    int least_s = 1 << 30, least_L = 1 << 30;
+
+    Runner(Group& g, char* ws, double eps_, hipStream_t s) : tb(g.tb), sums((float*)(ws + g.sums)), eps((float)eps_), st(s) {
+        for (int i = 0; i < tb.count; ++i) {
+            wide = wide && tb.mat[i].sp % 128 == 0 && tb.mat[i].Lp % 128 == 0;
+            single = single && tb.mat[i].sp == 64;
+            least_s = std::min(least_s, tb.mat[i].sp);
+            least_L = std::min(least_L, tb.mat[i].Lp);
         }
-        const bool last = step + len == steps;
-        int ea = exponent(lambda);
-        const float galpha = pow2(ea - 2 * ex);
-        const unsigned gram = number(tb, [&](const OMat& q) { return syms(q) * q.splits; });
-        if (first && NP == 1) run(k_orth_gram<TILE, 1>, gram, 1, product_lds<TILE, 1, 1>(), galpha, eps, 1);
-        else run(k_orth_gram<TILE, 2>, gram, 1, lds22, galpha, eps, (int)first);
-        run(k_orth_parts<TILE>, number(tb, [&](const OMat& q) { return q.splits > 1 ? syms(q) : 0; }), 1,
-            TILE * CP<TILE> * 4, galpha, eps, (int)first);
-        const unsigned sym = number(tb, syms);
-        int Q = -1, eq = 0;
-        double qb = 1.0;
-        for (int k = 0; k < len; ++k, ++step) {
-            const double* c = coef + 3 * step;
-            const Bound b = bound_of(c, lambda);
-            const int ep = exponent(b.p), et = exponent(b.p * lambda), en = exponent(b.lambda);
-            int P = 2;
-            while (P == Q) ++P;
-            const SymJob jp{0, 0, P, 0, (float)(c[2] * pow2(ep - 2 * ea)), (float)(c[1] * pow2(ep - ea)), (float)(c[0] * pow2(ep))};
-            run(k_orth_sym<TILE>, sym, 1, lds22, jp, jp);
-            qb = std::min(qb * b.p, 1e30);
-            const int eq2 = exponent(qb);
-            int Q2 = P;
-            if (Q >= 0) Q2 = 2 + 3 - (Q - 2) - (P - 2);
-            const SymJob jq{P, Q, Q2, -1, pow2(eq2 - ep - eq), 0.0f, 0.0f};
-            const SymJob jt{P, 0, 1, -1, pow2(et - ep - ea), 0.0f, 0.0f};
-            if (k + 1 < len) {
-                if (Q >= 0) run(k_orth_sym<TILE>, sym, 2, lds22, jt, jq);
-                else run(k_orth_sym<TILE>, sym, 1, lds22, jt, jt);
-                const SymJob ja{1, P, 0, -1, pow2(en - et - ep), 0.0f, 0.0f};
-                run(k_orth_sym<TILE>, sym, 1, lds22, ja, ja);
-            } else if (Q >= 0) {
-                run(k_orth_sym<TILE>, sym, 1, lds22, jq, jq);
-            }
-            eq = Q >= 0 ? eq2 : ep;
-            Q = Q2;
-            ea = en;
-            lambda = b.lambda;
-        }
-        const unsigned app = number(tb, [](const OMat& q) { return (q.sp / TILE) * (q.Lp / TILE); });
-        const int ex2 = exponent(sqrt(lambda));
-        constexpr int lds_a = product_lds<TILE, 2, NP>();
-        const float a = pow2((last ? 0 : ex2) - eq - ex);
-        if (last) {
-            if (first) run(k_orth_apply<TILE, NP, T, true>, app, 1, lds_a, Q, xt, a, eps, 1);
-            else run(k_orth_apply<TILE, 2, T, true>, app, 1, lds22, Q, xt, a, eps, 0);
-        } else {
-            if (first) run(k_orth_apply<TILE, NP, T, false>, app, 1, lds_a, Q, xt, a, eps, 1);
-            else run(k_orth_apply<TILE, 2, T, false>, app, 1, lds22, Q, xt, a, eps, 0);
-            xt ^= 1;
-        }
-        ex = ex2;
     }
-    return err;
-}
+
+    template <int THREADS = WG, typename K, typename... A>
+    void run(K kernel, unsigned grid, int lds, A... args) {
+        if (err != hipSuccess || grid == 0) return;
+        if (lds > 64 * 1024 && (err = ensure_dyn_lds((const void*)kernel, lds)) != hipSuccess) return;
+        hipLaunchKernelGGL(kernel, dim3(grid), dim3(THREADS), lds, st, tb, args...);
+        err = hipGetLastError();
+    }
+
+    template <int TILE, int P, bool GRAM>
+    void sym_t(SymLaunch& s, int jobs) {
+        constexpr int lds = product_lds<TILE, P, P>(), SLICES = TILE / JOIN_ROWS<TILE>;
+        auto tiles = [](const OMat& q) { const int t = q.sp / TILE; return t * (t + 1) / 2; };
+        s.sums = sums;
+        s.eps = eps;
+        s.tiles = (int)number(tb, tiles);
+        if (GRAM && (s.tiles < SLOTS || s.leave)) {
+            // the longer side is often much the longer: units over L of one length,
+            // of 256 at least, as many as the chip has slots for
+            long long cells = 0;  // in steps of 256 of L
+            for (int i = 0; i < tb.count; ++i) cells += (long long)tiles(tb.mat[i]) * tb.mat[i].batch * up(tb.mat[i].Lp, 256) / 256;
+            const long long len = std::max(1LL, (cells + SLOTS - 1) / SLOTS);
+            int unit = 0;
+            for (int i = 0; i < tb.count; ++i) {
+                OMat& q = tb.mat[i];
+                q.parts = (int)std::max(1LL, up(q.Lp, 256) / 256 / len);
+                q.unit0 = unit;
+                unit += tiles(q) * q.batch * q.parts;
+            }
+            s.whole = -1;
+            run<NT<TILE>>(k_orth_sym<TILE, P, GRAM>, number(tb, [&](const OMat& q) { return tiles(q) * q.parts; }), lds, s);
+            if (!s.leave)
+                run<NT<TILE>>(k_orth_join<TILE, GRAM>,
+                              number(tb, [&](const OMat& q) { return q.parts > 1 ? tiles(q) * SLICES : 0; }), 0, s);
+            return;
+        }
+        const Cut c = cut_of((long long)s.tiles * jobs, (GRAM ? least_L : least_s) / 256);
+        s.whole = c.whole;
+        s.parts = c.parts;
+        const int rest = s.tiles * jobs - c.whole;
+        run<NT<TILE>>(k_orth_sym<TILE, P, GRAM>, (unsigned)(c.whole + rest * c.parts), lds, s);
+        if (rest) run<NT<TILE>>(k_orth_join<TILE, GRAM>, (unsigned)(rest * SLICES), 0, s);
+    }
+    template <int P, bool GRAM>
+    void sym(SymLaunch s, int jobs) {
+        if (tile_of(sym_count(tb, 128) * jobs, wide) == 128) sym_t<128, P, GRAM>(s, jobs);
+        else sym_t<64, P, GRAM>(s, jobs);
+    }
+    void products(const SymJob& a) { sym<2, false>(SymLaunch{{a, a}}, 1); }
+    void products(const SymJob& a, const SymJob& b) { sym<2, false>(SymLaunch{{a, b}}, 2); }
+
+    template <int TILE, int P, bool LAST>
+    void apply_t(int Q, int xt, float alpha, int first) {
+        run<NT<TILE>>(k_orth_apply<TILE, P, T, LAST>, number(tb, [](const OMat& q) { return (q.sp / TILE) * (q.Lp / TILE); }),
+            product_lds<TILE, 2, P>(), Q, xt, alpha, eps, first);
+    }
+    template <int P, bool LAST>
+    void apply(int Q, int xt, float alpha, int first) {
+        long long n = 0;
+        for (int i = 0; i < tb.count; ++i) n += (long long)(tb.mat[i].sp / 128) * (tb.mat[i].Lp / 128) * tb.mat[i].batch;
+        if (tile_of(n, wide) == 128) apply_t<128, P, LAST>(Q, xt, alpha, first);
+        else apply_t<64, P, LAST>(Q, xt, alpha, first);
+    }
+
+    hipError_t go(int steps, const double* coef) {
+        if (!std::is_same<T, f16>::value) run(k_orth_amax<T>, number(tb, amax_wgs), 0);
+        run(k_orth_prep<T>, number(tb, prep_wgs), 0);
+        double lambda = 1.0;
+        int xt = 0, ex = 0, step = 0;  // X is stored times 2^ex (and 1 / norm_factor in the first block)
+        for (bool first = true; step < steps; first = false) {
+            int len = 0;
+            double growth = 1.0, l = lambda;
+            while (step + len < steps && len < STEP_MAX && (len == 0 || growth <= MAX_GROWTH)) {
+                const Bound b = bound_of(coef + 3 * (step + len), l);
+                growth *= b.p * b.p;
+                l = b.lambda;
+                ++len;
+            }
+            const bool last = step + len == steps;
+            int ea = exponent(lambda);
+            SymLaunch gram{{{0, 0, 0, -1, pow2(ea - 2 * ex), 0.0f, 0.0f}, {}}};
+            gram.first = first;
+            gram.leave = single;
+            Steps list{};
+            if (first) sym<NP, true>(gram, 1);
+            else sym<2, true>(gram, 1);
+            int Q = -1, eq = 0;  // Q: which of the workspace's matrices 2, 3, 4
+            double qb = 1.0;
+            for (int k = 0; k < len; ++k, ++step) {
+                const double* c = coef + 3 * step;
+                const Bound b = bound_of(c, lambda);
+                const int ep = exponent(b.p), et = exponent(b.p * lambda), en = exponent(b.lambda);
+                const int P = Q == 2 ? 3 : 2, Q2 = Q < 0 ? P : 9 - Q - P;
+                qb = std::min(qb * b.p, 1e30);
+                const int eq2 = Q < 0 ? ep : exponent(qb);
+                const SymJob jp{0, 0, P, 0, (float)(c[2] * pow2(ep - 2 * ea)), (float)(c[1] * pow2(ep - ea)),
+                                (float)(c[0] * pow2(ep))};
+                const SymJob jt{P, 0, 1, -1, pow2(et - ep - ea), 0.0f, 0.0f};
+                const SymJob ja{1, P, 0, -1, pow2(en - et - ep), 0.0f, 0.0f};
+                const SymJob jq{P, Q, Q2, -1, pow2(eq2 - ep - eq), 0.0f, 0.0f};
+                if (single) {
+                    list.one[k] = {jp.alpha, jp.beta, jp.gamma, jt.alpha, ja.alpha, jq.alpha};
+                } else {
+                    products(jp);
+                    if (k + 1 < len) {
+                        if (Q < 0) products(jt);
+                        else products(jt, jq);
+                        products(ja);
+                    } else if (Q >= 0) {
+                        products(jq);
+                    }
+                }
+                eq = eq2;
+                Q = Q2;
+                ea = en;
+                lambda = b.lambda;
+            }
+            if (single) {
+                list.len = len;
+                list.first = first;
+                list.Q = Q;
+                list.a0 = gram.job[0].alpha;
+                list.eps = eps;
+                list.sums = sums;
+                run<512>(k_orth_steps, number(tb, [](const OMat&) { return 1; }), STEPS_LDS, list);
+            }
+            const int ex2 = exponent(sqrt(lambda));
+            const float a = pow2((last ? 0 : ex2) - eq - ex);
+            if (last) {
+                if (first) apply<NP, true>(Q, xt, a, 1);
+                else apply<2, true>(Q, xt, a, 0);
+            } else {
+                if (first) apply<NP, false>(Q, xt, a, 1);
+                else apply<2, false>(Q, xt, a, 0);
+                xt ^= 1;
+            }
+            ex = ex2;
+        }
+        return err;
+    }
+};
 
 template <typename T>
 hipError_t orth_t(const OrthMat* mats, int count, int steps, const double* coef, double eps, Ws ws, hipStream_t st) {
@@ -655,11 +1078,18 @@ hipError_t orth_t(const OrthMat* mats, int count, int steps, const double* coef,
             const OrthMat& q = mats[g.entry[k]];
             o.g = (const T*)q.g + g.first[k] * q.bstride;
             o.o = (T*)q.o + g.first[k] * q.bstride_o;
+            o.scaled = !std::is_same<T, f16>::value;
             o.ws = at;
             at += o.ws_one * o.batch;
+            constexpr long long V = 16 / sizeof(T);
+            auto aligned = [](const void* p, long long ld, long long stride) {
+                return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % V == 0 && stride % V == 0;
+            };
+            // (a single row needs no distance)
+            o.vec = (aligned(o.g, o.m > 1 ? o.ld : 0, o.bstride) ? 1 : 0) |
+                    (aligned(o.o, o.m > 1 ? o.ld_o : 0, o.bstride_o) ? 2 : 0);
         }
-        const hipError_t e = g.tile == 128 ? orth_group<T, 128>(g, steps, coef, eps, st)
-                                           : orth_group<T, 64>(g, steps, coef, eps, st);
+        const hipError_t e = Runner<T>(g, (char*)ws.p, eps, st).go(steps, coef);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
