@@ -1,0 +1,299 @@
+"""GPU parity of the Newton-Schulz orthogonalisation against the iteration in 64
+bits on the CPU.
+
+Tolerances (2-norm of the difference over the 2-norm of the result).  The result
+is rounded once, which is at most half a step a value: 2^-8 (bf16), 2^-11 (fp16),
+2^-24 (fp32).  Within the iteration matrices carry 22 bits and a sign and products
+drop lo times lo, together below 2^-21 a product and matrix, and sums are fp32.
+In directions of small singular values an error of A grows by a^2 = 11.9 a step
+until the block ends: 11.9 for fp32, 141 for fp16, 2e4 for bf16 (blocks of 2, 3
+and 5 steps), and p = a + b A + .. turns an error d of A into b / a d < 2 d of the
+result.  A has a 2-norm of at most 1, its error one of at most 2^-21 in the
+2-norm (rounding errors of one sign in a row would give sqrt(s) of that, and
+have signs of their own), in three to five blocks of up to four products:
+  fp32 5 * 4 * 2 * 11.9 * 2^-21 = 2.3e-4,  fp16 2 * 6 * 2 * 141 * 2^-21 = 1.6e-3,
+  bf16 2 * 2e4 * 2^-21 = 1.9e-2
+bound the worst spectrum.  The gradients here have directions between 1 and 1e-3
+of the largest with |A| below 0.3, errors of random sign and so a hundredth of
+that; what is asserted is a tenth, plus the rounding: fp32 2e-5, fp16 2^-11 + 2e-4,
+bf16 2^-8 + 2e-3.
+"""
+from __future__ import annotations
+
+import math
+
+import pytest
+import torch
+
+import paper_2011_12025_amd as sb
+from parity_util import log
+
+pytestmark = pytest.mark.gpu
+
+DT = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+TOL = {"f32": 2e-5, "f16": 2.0 ** -11 + 2e-4, "bf16": 2.0 ** -8 + 2e-3}
+ABC = (3.4445, -4.7750, 2.0315)
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _need_gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2011_12025_amd._binding as b
+    b.lib()
+
+
+def reference(g, steps=5, coef=None, eps=1e-7):
+    """g [m, n] on any device -> 64 bits on the CPU."""
+    x = g.detach().double().cpu()
+    flip = x.shape[0] > x.shape[1]
+    x = x.t() if flip else x
+    x = x / (x.norm() + eps)
+    for i in range(steps):
+        a, b, c = ABC if coef is None else coef[i]
+        A = x @ x.t()
+        x = a * x + (b * A + c * (A @ A)) @ x
+    return x.t() if flip else x
+
+
+def gradient(m, n, dtype, gen, scale=1e-3):
+    r = max(1, min(m, n) // 8)
+    g = (torch.randn(m, r, generator=gen) * torch.arange(1, r + 1).rsqrt()) @ torch.randn(r, n, generator=gen)
+    return ((g + 0.5 * torch.randn(m, n, generator=gen)) * scale).to(DT[dtype]).cuda()
+
+
+def near(got, ref, tol, what):
+    got = got.double().cpu().reshape(ref.shape)
+    if bool(ref.isnan().all()):  # an update that is not finite (1e4 times a normal value can pass fp16's end)
+        assert bool(got.isnan().all()), what
+        return
+    assert bool(got.isfinite().all()), f"{what}: not finite"
+    off = (got - ref).norm().item() / max(ref.norm().item(), 1e-300)
+    assert off <= tol, f"{what}: {off:.2e} off, {tol:.2e} allowed"
+
+
+SHAPES = [(1, 1), (1, 5), (7, 1), (2, 3), (5, 4), (33, 64), (64, 33), (64, 64), (65, 64), (63, 200), (64, 576), (576, 64),
+          (100, 130), (128, 1152), (129, 127), (300, 1000), (1000, 300), (257, 257), (64, 4097), (5000, 40), (700, 701),
+          (1025, 2050)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("m,n", SHAPES)
+def test_shapes(m, n, dtype):
+    log(f"[orthogonalize] {m} x {n} {dtype}")
+    g = gradient(m, n, dtype, torch.Generator().manual_seed(m + 3 * n))
+    near(sb.orthogonalize(g), reference(g), TOL[dtype], f"{m} x {n}")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_tiles_past_one_round(dtype):
+    """More tiles than the chip takes at once: whole rounds and a split remainder.
+    The matrix repeats a small one along its diagonal, so 64 bits need only that."""
+    log(f"[orthogonalize] diagonal blocks {dtype}")
+    k, b = 16, 256
+    g = gradient(b, b, dtype, torch.Generator().manual_seed(5))
+    big = torch.zeros(k * b, k * b, dtype=g.dtype, device="cuda")
+    for i in range(k):
+        big[i * b:(i + 1) * b, i * b:(i + 1) * b] = g
+    out = sb.orthogonalize(big)
+    # of the whole |G| = sqrt(k) |g|
+    x = g.double().cpu() / (math.sqrt(k) * g.double().norm().cpu() + 1e-7)
+    for _ in range(5):
+        A = x @ x.t()
+        x = ABC[0] * x + (ABC[1] * A + ABC[2] * (A @ A)) @ x
+    # the norm of one block's error is the whole's over sqrt(k)
+    for i in (0, 7, 15):
+        near(out[i * b:(i + 1) * b, i * b:(i + 1) * b], x, TOL[dtype], f"block {i}")
+        out[i * b:(i + 1) * b, i * b:(i + 1) * b] = 0
+    assert out[:b].abs().max().item() == 0.0 and out[-b:].abs().max().item() == 0.0
+
+
+def later_growth(g, steps):
+    """By how much an error of a singular value after step 5 or a later one is
+    multiplied until the end: the largest product of |f'(sigma)| over the steps
+    left.  f has no stable point near 1 (f(0.868) = 0.868 with f' = -1.58, and f'(1.2)
+    = 3.9), so with these coefficients an iteration that goes on amplifies
+    every rounding; five steps end before that."""
+    a, b, c = ABC
+    s = torch.linalg.svdvals(g.double().cpu())
+    s = s / (s.norm() + 1e-7)
+    slopes = []
+    for _ in range(steps):
+        slopes.append((a + 3 * b * s ** 2 + 5 * c * s ** 4).abs())
+        s = a * s + b * s ** 3 + c * s ** 5
+    worst, grown = 1.0, torch.ones_like(s)
+    for d in reversed(slopes[5:]):
+        grown = grown * d
+        worst = max(worst, grown.max().item())
+    return worst
+
+
+@pytest.mark.parametrize("steps", [1, 2, 3, 4, 6, 9, 20])
+@pytest.mark.parametrize("m,n", [(40, 90), (200, 150)])
+def test_steps(m, n, steps):
+    log(f"[orthogonalize] {steps} steps {m} x {n}")
+    gen = torch.Generator().manual_seed(steps)
+    for dtype in ("f32", "f16", "bf16"):
+        g = gradient(m, n, dtype, gen)
+        grown = later_growth(g, steps) * max(1, steps / 5)  # (each block adds an error of its own)
+        got = sb.orthogonalize(g, steps=steps)
+        if TOL[dtype] * grown < 0.1:
+            near(got, reference(g, steps), TOL[dtype] * grown, f"{steps} {dtype}")
+        # whatever the rounding, f keeps its singular values in [0.67, 1.21]
+        s = torch.linalg.svdvals(got.double().cpu())
+        assert steps < 9 or (s.min() > 0.6 and s.max() < 1.25)
+
+
+def test_many_steps_that_converge():
+    """32 steps of the cubic x (1.5 - 0.5 x^2), whose point at 1 is stable: the nearest orthogonal matrix."""
+    gen = torch.Generator().manual_seed(4)
+    for m, n in [(40, 90), (200, 150)]:
+        for dtype in ("f32", "f16", "bf16"):
+            g = gradient(m, n, dtype, gen)
+            u, _, v = torch.linalg.svd(g.double().cpu(), full_matrices=False)
+            near(sb.orthogonalize(g, steps=32, coefficients=(1.5, -0.5, 0.0)), u @ v, TOL[dtype], f"{m} x {n} {dtype}")
+
+
+def test_coefficients_of_every_step():
+    gen = torch.Generator().manual_seed(2)
+    coef = [(4.0, -6.0, 2.5), (3.9, -5.5, 2.2), (2.0, -1.5, 0.5), (1.875, -1.25, 0.375), (1.5, -0.5, 0.0)]
+    for m, n in [(50, 70), (300, 200)]:
+        for dtype in ("f32", "bf16"):
+            g = gradient(m, n, dtype, gen)
+            out = sb.orthogonalize(g, steps=5, coefficients=coef)
+            near(out, reference(g, 5, coef), TOL[dtype], f"{m} x {n} {dtype}")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_lists_batches_filters_and_views(dtype):
+    log(f"[orthogonalize] a list of all forms, {dtype}")
+    gen = torch.Generator().manual_seed(7)
+    cl = torch.channels_last
+    w = gradient(64, 64 * 9, dtype, gen).reshape(64, 64, 3, 3)
+    wide = gradient(90, 333, dtype, gen)
+    updates = [w, w.contiguous(memory_format=cl), gradient(128, 64, dtype, gen).reshape(128, 64, 1, 1),
+               torch.stack([gradient(40, 70, dtype, gen) for _ in range(5)]), wide[3:80, 5:300], wide.t(),
+               gradient(33, 40, dtype, gen)[::2], torch.stack([gradient(130, 30, dtype, gen) for _ in range(3)])[:, 1:, :-3],
+               gradient(17, 90, dtype, gen)] + [gradient(20 + i, 60, dtype, gen) for i in range(40)]
+    outs = sb.orthogonalize(updates)
+    assert len(outs) == len(updates)
+    for i, (g, o) in enumerate(zip(updates, outs)):
+        assert o.shape == g.shape and o.dtype == g.dtype
+        flat = g.reshape(1, g.shape[0], -1) if g.dim() != 3 else g
+        for b in range(flat.shape[0]):
+            near(o.reshape(flat.shape)[b], reference(flat[b]), TOL[dtype], f"update {i}, matrix {b}")
+    assert outs[1].is_contiguous(memory_format=cl)
+    # a filter alone, in a list and in another format: the same values (columns in another order)
+    torch.testing.assert_close(outs[0].float(), outs[1].float(), rtol=0, atol=TOL[dtype] * 4)
+    into = [torch.zeros_like(u) for u in updates]
+    sb.orthogonalize(updates, out=into)
+    assert all(torch.equal(a, b) for a, b in zip(into, outs))
+
+
+def test_out_rows_leave_what_lies_between():
+    gen = torch.Generator().manual_seed(3)
+    g = gradient(70, 50, "f32", gen)
+    big = torch.full((70, 64), 9.0, device="cuda")
+    sb.orthogonalize(g, out=big[:, 3:53])
+    assert bool((big[:, :3] == 9).all()) and bool((big[:, 53:] == 9).all())
+    near(big[:, 3:53], reference(g), TOL["f32"], "columns of a wider buffer")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("m,n", [(48, 100), (150, 260)])
+def test_zeros_ranks_and_scales(m, n, dtype):
+    """Zeros, zero rows, one direction, large and tiny values, NaN and infinity."""
+    log(f"[orthogonalize] odd values {m} x {n} {dtype}")
+    gen = torch.Generator().manual_seed(m)
+    assert sb.orthogonalize(torch.zeros(m, n, dtype=DT[dtype], device="cuda")).abs().max().item() == 0.0
+    assert sb.orthogonalize(torch.zeros(m, n, dtype=DT[dtype], device="cuda"), eps=0.0).abs().max().item() == 0.0
+    g = gradient(m, n, dtype, gen)
+    g[3:9] = 0
+    near(sb.orthogonalize(g), reference(g), TOL[dtype], "zero rows")
+    one = torch.outer(torch.randint(1, 4, (m,), generator=gen).float(), torch.randint(1, 4, (n,), generator=gen).float())
+    one = one.to(DT[dtype]).cuda()  # exactly of rank one: sigma = 1, the worst |A|
+    near(sb.orthogonalize(one), reference(one), 4 * TOL[dtype], "rank one")
+    for scale in ((1e-3, 1e3, 1e4) if dtype == "f16" else (1e-30, 1e-20, 1e20, 1e30)):
+        g = gradient(m, n, "f32", gen, 1.0).mul(scale).to(DT[dtype])
+        # (fp16 subnormals have fewer bits, but those are the update's own)
+        near(sb.orthogonalize(g, eps=0.0), reference(g, eps=0.0), TOL[dtype], f"scale {scale}")
+    tiny = gradient(m, n, dtype, gen, 1e-6 if dtype == "f16" else 1e-9)
+    near(sb.orthogonalize(tiny, eps=1e-3), reference(tiny, eps=1e-3), 2 * TOL[dtype], "eps counts")
+    for bad in (math.nan, math.inf):
+        g = gradient(m, n, dtype, gen)
+        g[m // 2, n // 3] = bad
+        assert bool(sb.orthogonalize(g).isnan().all())
+    # of a list, one alone
+    good = gradient(m, n, dtype, gen)
+    a, b = sb.orthogonalize([g, good])
+    assert bool(a.isnan().all()) and torch.equal(b, sb.orthogonalize(good))
+
+
+def test_empty_updates_and_lists():
+    assert sb.orthogonalize([]) == []
+    assert sb.orthogonalize(torch.empty(0, 5, device="cuda")).shape == (0, 5)
+    a, b = sb.orthogonalize([torch.empty(3, 0, 7, device="cuda"), torch.ones(2, 3, device="cuda")])
+    assert a.shape == (3, 0, 7) and bool(b.isfinite().all())
+
+
+@pytest.mark.parametrize("bad", ["steps", "steps32", "coefficients", "nan", "eps", "types", "vector", "strides", "out shape",
+                                 "overlap", "workspace", "cpu", "double"])
+def test_refusals(bad):
+    g = torch.randn(20, 30, device="cuda")
+    with pytest.raises((ValueError, TypeError, RuntimeError)):
+        if bad == "steps":
+            sb.orthogonalize(g, steps=0)
+        elif bad == "steps32":
+            sb.orthogonalize(g, steps=33)
+        elif bad == "coefficients":
+            sb.orthogonalize(g, coefficients=[(1, 2, 3)] * 4)
+        elif bad == "nan":
+            sb.orthogonalize(g, coefficients=(math.nan, 0.0, 0.0))
+        elif bad == "eps":
+            sb.orthogonalize(g, eps=-1.0)
+        elif bad == "types":
+            sb.orthogonalize([g, g.half()])
+        elif bad == "vector":
+            sb.orthogonalize(g[0])
+        elif bad == "strides":
+            sb.orthogonalize(torch.randn(20, 60, device="cuda")[:, ::2])
+        elif bad == "out shape":
+            sb.orthogonalize(g, out=torch.empty(30, 20, device="cuda"))
+        elif bad == "overlap":
+            sb.orthogonalize(g, out=g)
+        elif bad == "workspace":
+            sb.orthogonalize(g, workspace=torch.empty(1000, dtype=torch.uint8, device="cuda"))
+        elif bad == "cpu":
+            sb.orthogonalize(g.cpu())
+        elif bad == "double":
+            sb.orthogonalize(g.double())
+
+
+def test_stream_capture_workspace_and_reproducibility():
+    """A caller's workspace, a side stream, a graph replayed among eager work on other values: the same bits."""
+    gen = torch.Generator().manual_seed(12)
+    gs = [gradient(64, 300, "bf16", gen), gradient(200, 150, "bf16", gen)]
+    small = [gradient(30, 40, "bf16", gen)]
+    ws = torch.empty(max(sb.orthogonalize_workspace_size(gs), sb.orthogonalize_workspace_size(small)) + 256,
+                     dtype=torch.uint8, device="cuda").fill_(255)
+    first = [o.clone() for o in sb.orthogonalize(gs, workspace=ws)] + [sb.orthogonalize(small, workspace=ws)[0].clone()]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        other = sb.orthogonalize(gs) + sb.orthogonalize(small)
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(a, b) for a, b in zip(first, other))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = sb.orthogonalize(gs, workspace=ws) + sb.orthogonalize(small, workspace=ws)
+    keep = [g.clone() for g in gs]
+    for i in range(4):
+        for g, k in zip(gs, keep):
+            g.copy_(k if i % 2 == 0 else k.flip(0))
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = sb.orthogonalize(gs) + sb.orthogonalize(small)
+        torch.cuda.synchronize()
+        for x, y, w in zip(out, eager, first):
+            assert torch.equal(x, y)
+            assert i % 2 or torch.equal(x, w)
