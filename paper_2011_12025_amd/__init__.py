@@ -12,7 +12,6 @@ convolution that applies the same filters to both block stacks.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import functools
 
@@ -663,72 +662,80 @@ def layer_backward(x: torch.Tensor, mask: torch.Tensor, bs: int, weight: torch.T
 # and the update of a filter from its gradient
 # ---------------------------------------------------------------------------
 
-@contextlib.contextmanager
-def _nothing():
-    yield
-
-
-def _on(t: torch.Tensor):
-    """The device of t as the current one for a call that launches there."""
+def _device_of(t: torch.Tensor) -> int:
     index = t.get_device()
     if index < 0:
         raise ValueError(f"expected a cuda tensor, but got one on {t.device}")
-    return _nothing() if index == torch.cuda.current_device() else torch.cuda.device(index)
+    return index
 
 
-def _scores(t: torch.Tensor, what: str = "logits"):
+# The device that calls go to now (torch.cuda.current_device without its check
+# whether CUDA has begun: there is a tensor on it).
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _scores(shape, stride, what: str = "logits"):
     """(layout, N, C, H, W, C_buf) of class scores: a map [N, C, H, W] in either
     memory format or rows [R, C] / [B, S, C], whose classes may be the first C
     of a wider buffer (a slice of its channels)."""
-    if t.dim() == 4:
-        N, C, H, W = t.shape
-        sn, sc, sh, sw = t.stride()
+    found = None
+    if len(shape) == 4:
+        N, C, H, W = shape
+        sn, sc, sh, sw = stride
         if C == 1 or sc == 1:  # channels last
             c = sw if W > 1 else sh if H > 1 else sn if N > 1 else C
-            if c >= C and (H == 1 or sh == W * c) and (N == 1 or sn == H * W * c):
-                return _b.SB_NHWC, N, C, H, W, c
+            if c >= C and (H <= 1 or sh == W * c) and (N <= 1 or sn == H * W * c):
+                found = _b.SB_NHWC, N, C, H, W, c
         P = H * W
-        if (W == 1 or sw == 1) and (H == 1 or sh == W) and (C == 1 or sc == P):
-            if N == 1:
-                return _b.SB_NCHW, N, C, H, W, C
-            if sn % P == 0 and sn // P >= C:
-                return _b.SB_NCHW, N, C, H, W, sn // P
-        raise ValueError(f"{what} must be contiguous or channels_last, or the first channels of such a map")
-    if t.dim() == 2 or t.dim() == 3:
-        C = t.shape[-1]
-        rows = t.shape[0] if t.dim() == 2 else t.shape[0] * t.shape[1]
-        lead = [(n, s) for n, s in zip(t.shape[:-1], t.stride()[:-1]) if n > 1]
+        if found is None and (W <= 1 or sw == 1) and (H <= 1 or sh == W) and (C == 1 or sc == P):
+            if N <= 1:
+                found = _b.SB_NCHW, N, C, H, W, C
+            elif P and sn % P == 0 and sn // P >= C:
+                found = _b.SB_NCHW, N, C, H, W, sn // P
+        if found is None and 0 in shape:
+            found = _b.SB_NCHW, N, C, H, W, C
+        if found is None:
+            raise ValueError(f"{what} must be contiguous or channels_last, or the first channels of such a map")
+    elif len(shape) == 2 or len(shape) == 3:
+        C = shape[-1]
+        rows = shape[0] if len(shape) == 2 else shape[0] * shape[1]
+        lead = [(n, s) for n, s in zip(shape[:-1], stride[:-1]) if n > 1]
         c = lead[-1][1] if lead else C
-        if (C == 1 or t.stride(-1) == 1) and c >= C and (len(lead) < 2 or lead[0][1] == lead[1][0] * c):
-            return _b.SB_NHWC, rows, C, 1, 1, c
-        raise ValueError(f"{what} must be rows of contiguous scores at one distance")
-    raise ValueError(f"{what} must be [rows, classes], [batch, rows, classes] or [N, classes, H, W]")
-
-
-def _sizes(t: torch.Tensor):
-    s = _scores(t)
-    if max(s) >= 1 << 31:
+        if 0 in shape:
+            c = C
+        elif not ((C == 1 or stride[-1] == 1) and c >= C and (len(lead) < 2 or lead[0][1] == lead[1][0] * c)):
+            raise ValueError(f"{what} must be rows of contiguous scores at one distance")
+        found = _b.SB_NHWC, rows, C, 1, 1, c
+    else:
+        raise ValueError(f"{what} must be [rows, classes], [batch, rows, classes] or [N, classes, H, W]")
+    if max(found) >= 1 << 31:
         raise ValueError("at most 2^31 - 1 rows, classes and channels")
-    return s
+    if found[2] == 0:
+        raise ValueError("no classes")
+    return found
 
 
-def _row_shapes(t: torch.Tensor):
-    """Shape of one value a row of scores t, and of k a row (as a function)."""
-    if t.dim() == 4:
-        return (t.shape[0], *t.shape[2:]), lambda k: (t.shape[0], k, *t.shape[2:])
-    return tuple(t.shape[:-1]), lambda k: (*t.shape[:-1], k)
+@functools.lru_cache(maxsize=4096)
+def _score_plan(device: int, dt: int, topk: int, shape, stride):
+    """What a call on scores of these sizes needs to know, remembered: _scores,
+    the shapes of one value a row and of topk a row, the workspace."""
+    s = _scores(shape, stride)
+    layout, N, C, H, W, c_buf = s
+    if not 0 <= topk <= min(64, C):
+        raise ValueError(f"topk must be in [0, min(64, classes)], got {topk}")
+    one = (N, H, W) if len(shape) == 4 else tuple(shape[:-1])
+    many = (N, topk, H, W) if len(shape) == 4 else (*one, topk)
+    need = _query("segblocks_log_probs_workspace_size", dt, layout, N, C, H, W, c_buf, topk) if N * H * W else 0
+    return (*s, one, many, _fmt(layout) if len(shape) == 4 else torch.contiguous_format, need)
 
 
-def _row_values(v, like: torch.Tensor, shape, dtype: torch.dtype, what: str, layout=None):
-    """v (or None), checked to hold one value a row (or top_* values in the
-    call's memory format), dense."""
-    if v is None:
-        return None
-    if v.dtype != dtype or tuple(v.shape) != tuple(shape):
+def _row_values(v, device: int, shape, dtype: torch.dtype, what: str, fmt=torch.contiguous_format):
+    """v, checked to hold the values of every row, dense in the memory format."""
+    if v.dtype != dtype or v.shape != shape:
         raise ValueError(f"{what} must be a {dtype} tensor of shape {tuple(shape)}, got {v.dtype} {tuple(v.shape)}")
-    if v.device != like.device:
-        raise ValueError(f"{what} is on {v.device}, the scores on {like.device}")
-    return v.contiguous() if layout is None or v.dim() != 4 else v.contiguous(memory_format=_fmt(layout))
+    if v.get_device() != device:
+        raise ValueError(f"{what} is on {v.device}, the scores on cuda:{device}")
+    return v if v.is_contiguous(memory_format=fmt) else v.contiguous(memory_format=fmt)
 
 
 def log_probs_workspace_size(dtype: torch.dtype, layout: int, N: int, C: int, H: int, W: int, C_buf: int,
@@ -751,32 +758,30 @@ def log_probs(logits: torch.Tensor, labels=None, topk: int = 0, entropy: bool = 
     or [..., topk]; float32 and int32, None for what is not asked for.  Equal
     scores rank by class, lower first.  ``workspace`` as in block_conv3x3, sized
     by log_probs_workspace_size()."""
-    layout, N, C, H, W, c_buf = _sizes(logits)
-    one, many = _row_shapes(logits)
-    labels = _row_values(labels, logits, one, torch.int64, "labels")
+    device, dt = _device_of(logits), _dt(logits)
+    if device != _current_device():
+        with torch.cuda.device(device):
+            return log_probs(logits, labels, topk, entropy, ignore, workspace)
+    layout, N, C, H, W, c_buf, one, many, fmt, need = _score_plan(device, dt, topk, logits.shape, logits.stride())
     dev = logits.device
-
-    def new(dtype=torch.float32):
-        return torch.empty(one, dtype=dtype, device=dev)
-
-    def new_top(dtype):
-        if logits.dim() == 4:
-            return torch.empty(many(topk), dtype=dtype, device=dev, memory_format=_fmt(layout))
-        return torch.empty(many(topk), dtype=dtype, device=dev)
-
-    if topk < 0 or topk > min(64, C):
-        raise ValueError(f"topk must be in [0, min(64, classes)], got {topk}")
-    dt = _dt(logits)
-    with _on(logits):
-        logp, lse, ent = None if labels is None else new(), new(), new() if entropy else None
-        tl, ti = (new_top(torch.float32), new_top(torch.int32)) if topk else (None, None)
-        if logits.numel():
-            need = _need("segblocks_log_probs_workspace_size", dt, layout, N, C, H, W, c_buf, topk)
-            wp, wn, _keep = _ws(need, dev, workspace)
-            _b.call("segblocks_log_probs", _ptr(logits), dt, layout, N, C, H, W, c_buf, _ptr(labels), ignore, topk,
-                    _ptr(logp), _ptr(lse), _ptr(ent), _ptr(tl), _ptr(ti), wp, wn, _stream(logits))
-        elif C == 0:
-            raise ValueError("no classes")
+    empty, f32 = torch.empty, torch.float32
+    lse = empty(one, dtype=f32, device=dev)
+    logp = ent = tl = ti = p_labels = p_logp = p_ent = p_tl = p_ti = None
+    if labels is not None:
+        labels = _row_values(labels, device, one, torch.int64, "labels")
+        logp = empty(one, dtype=f32, device=dev)
+        p_labels, p_logp = labels.data_ptr(), logp.data_ptr()
+    if entropy:
+        ent = empty(one, dtype=f32, device=dev)
+        p_ent = ent.data_ptr()
+    if topk:
+        tl = empty(many, dtype=f32, device=dev, memory_format=fmt)
+        ti = empty(many, dtype=torch.int32, device=dev, memory_format=fmt)
+        p_tl, p_ti = tl.data_ptr(), ti.data_ptr()
+    if N * H * W:
+        wp, wn, _keep = _ws(need, dev, workspace) if need else (None, 0, None)
+        _b.call("segblocks_log_probs", logits.data_ptr(), dt, layout, N, C, H, W, c_buf, p_labels, ignore, topk, p_logp,
+                lse.data_ptr(), p_ent, p_tl, p_ti, wp, wn, _raw_stream(device))
     return logp, lse, ent, tl, ti
 
 
@@ -788,46 +793,53 @@ def log_probs_backward(logits: torch.Tensor, labels, lse: torch.Tensor, d_logp=N
     entropy and top_index.  ``out``: a tensor shaped and ordered like ``logits``
     to write to, such as the first channels of the map that a layer's backward
     pass takes (its other channels are left as they are)."""
-    layout, N, C, H, W, c_buf = _sizes(logits)
-    one, many = _row_shapes(logits)
-    labels = _row_values(labels, logits, one, torch.int64, "labels")
-    f32 = torch.float32
-    lse, d_logp, entropy, d_entropy = (_row_values(v, logits, one, f32, n) for v, n in (
-        (lse, "lse"), (d_logp, "d_logp"), (entropy, "entropy"), (d_entropy, "d_entropy")))
+    device, dt = _device_of(logits), _dt(logits)
+    if device != _current_device():
+        with torch.cuda.device(device):
+            return log_probs_backward(logits, labels, lse, d_logp, entropy, d_entropy, top_index, d_top, ignore, out)
     topk = 0
     if d_top is not None:
         if top_index is None:
             raise ValueError("d_top needs top_index")
         topk = top_index.shape[1 if logits.dim() == 4 else -1]
-        top_index = _row_values(top_index, logits, many(topk), torch.int32, "top_index", layout)
-        d_top = _row_values(d_top, logits, many(topk), f32, "d_top", layout)
-        if topk == 0:
-            top_index = d_top = None
+    layout, N, C, H, W, c_buf, one, many, fmt, _ = _score_plan(device, dt, topk, logits.shape, logits.stride())
+    f32 = torch.float32
+    lse = _row_values(lse, device, one, f32, "lse")
+    p_labels = p_logp = p_ent = p_dent = p_index = p_dtop = None
+    # (the names keep what _row_values made dense until the call)
+    if d_logp is not None:
+        if labels is None:
+            raise ValueError("d_logp needs labels")
+        labels, d_logp = _row_values(labels, device, one, torch.int64, "labels"), _row_values(d_logp, device, one, f32, "d_logp")
+        p_labels, p_logp = labels.data_ptr(), d_logp.data_ptr()
+    if d_entropy is not None:
+        if entropy is None:
+            raise ValueError("d_entropy needs entropy")
+        entropy = _row_values(entropy, device, one, f32, "entropy")
+        d_entropy = _row_values(d_entropy, device, one, f32, "d_entropy")
+        p_ent, p_dent = entropy.data_ptr(), d_entropy.data_ptr()
+    if topk:
+        top_index = _row_values(top_index, device, many, torch.int32, "top_index", fmt)
+        d_top = _row_values(d_top, device, many, f32, "d_top", fmt)
+        p_index, p_dtop = top_index.data_ptr(), d_top.data_ptr()
+    if out is None:
+        out, c_out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device, memory_format=fmt), C
     else:
-        top_index = None
-    with _on(logits):
-        if out is None:
-            out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device,
-                              memory_format=_fmt(layout) if logits.dim() == 4 else torch.contiguous_format)
         if out.dtype != logits.dtype or out.shape != logits.shape or out.device != logits.device:
             raise ValueError("out must have the scores' type, shape and device")
         c_out = _buf_channels(out, layout)
-        if logits.numel():
-            _b.call("segblocks_log_probs_backward", _ptr(logits), _dt(logits), layout, N, C, H, W, c_buf, _ptr(labels),
-                    ignore, _ptr(lse), _ptr(d_logp), _ptr(entropy), _ptr(d_entropy), topk, _ptr(top_index), _ptr(d_top),
-                    c_out, _ptr(out), _stream(logits))
+    if N * H * W:
+        _b.call("segblocks_log_probs_backward", logits.data_ptr(), dt, layout, N, C, H, W, c_buf, p_labels, ignore,
+                lse.data_ptr(), p_logp, p_ent, p_dent, topk, p_index, p_dtop, c_out, out.data_ptr(), _raw_stream(device))
     return out
 
 
 def _buf_channels(t: torch.Tensor, layout: int) -> int:
     """C_buf of a tensor of scores that has to be in `layout`."""
-    got, N, C, H, W, c = _scores(t, "out")
-    if c >= 1 << 31:
-        raise ValueError("at most 2^31 - 1 channels")
-    if got != layout:
-        # one of the two where both describe the memory: a single pixel, or a single class
-        if not (H * W == 1 or (C == 1 and c == 1)):
-            raise ValueError("out must share the scores' memory format")
+    got, N, C, H, W, c = _scores(t.shape, t.stride(), "out")
+    # (a single pixel, or a single class, is in both)
+    if got != layout and not (H * W == 1 or (C == 1 and c == 1)):
+        raise ValueError("out must share the scores' memory format")
     return c
 
 
@@ -894,7 +906,11 @@ def orthogonalize(updates, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315
     if not updates:
         return []
     ref = updates[0]
-    dt = _dt(ref)
+    device, dt = _device_of(ref), _dt(ref)
+    if device != _current_device():
+        with torch.cuda.device(device):
+            o = orthogonalize(updates, steps, coefficients, eps, [out] if single and out is not None else out, workspace)
+            return o[0] if single else o
     for t in updates:
         if t.dtype != ref.dtype or t.device != ref.device:
             raise ValueError("the updates of a call share the type and the device")
@@ -905,23 +921,22 @@ def orthogonalize(updates, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315
         coef = coef * steps
     if len(coef) != 3 * steps:
         raise ValueError("coefficients must be (a, b, c), or one such triple for every step")
-    with _on(ref):
-        if out is None:
-            outs = [torch.empty_like(t) for t in updates]
-        else:
-            outs = [out] if isinstance(out, torch.Tensor) else list(out)
-            if len(outs) != len(updates) or any(o.shape != t.shape or o.dtype != t.dtype or o.device != t.device or
-                                                (t.dim() == 4 and layout_of(o) != layout_of(t))
-                                                for o, t in zip(outs, updates)):
-                raise ValueError("out must have the updates' shapes, type, device and memory format")
-        some = [(t, o) for t, o in zip(updates, outs) if t.numel()]
-        if some:
-            mats = _matrices(*zip(*some))
-            n = ctypes.c_size_t(0)
-            _b.call("segblocks_orthogonalize_workspace_size", mats, len(some), dt, ctypes.byref(n))
-            wp, wn, _keep = _ws(int(n.value), ref.device, workspace)
-            _b.call("segblocks_orthogonalize", mats, len(some), dt, steps, (ctypes.c_double * len(coef))(*coef),
-                    float(eps), wp, wn, _stream(ref))
+    if out is None:
+        outs = [torch.empty_like(t) for t in updates]
+    else:
+        outs = [out] if isinstance(out, torch.Tensor) else list(out)
+        if len(outs) != len(updates) or any(o.shape != t.shape or o.dtype != t.dtype or o.device != t.device or
+                                            (t.dim() == 4 and layout_of(o) != layout_of(t))
+                                            for o, t in zip(outs, updates)):
+            raise ValueError("out must have the updates' shapes, type, device and memory format")
+    some = [(t, o) for t, o in zip(updates, outs) if t.numel()]
+    if some:
+        mats = _matrices(*zip(*some))
+        n = ctypes.c_size_t(0)
+        _b.call("segblocks_orthogonalize_workspace_size", mats, len(some), dt, ctypes.byref(n))
+        wp, wn, _keep = _ws(int(n.value), ref.device, workspace)
+        _b.call("segblocks_orthogonalize", mats, len(some), dt, steps, (ctypes.c_double * len(coef))(*coef),
+                float(eps), wp, wn, _raw_stream(device))
     return outs[0] if single else outs
 
 

@@ -103,27 +103,8 @@ __device__ __forceinline__ u64 lane_key(u64 k, int lane) {
 }
 
 struct TopList {
-    u64 key;    // this lane's
-    u64 last;   // the topk-th
-    float cut;  // its score: below it nothing can enter (NaN while the list has room)
-
-    __device__ __forceinline__ void close(int topk) {
-        last = lane_key(key, topk - 1);
-        cut = last ? key_score(last) : NAN;
-    }
-    // one key a lane (0: none), ranked by counting the larger ones
-    __device__ __forceinline__ void start(u64 k, int topk) {
-        int rank = 0;
-#pragma unroll 8
-        for (int l = 0; l < 64; ++l) {
-            const u64 o = lane_key(k, l);
-            rank += o > k || (o == k && l < lane_id()) ? 1 : 0;
-        }
-        const uint32_t hi = (uint32_t)__builtin_amdgcn_ds_permute(rank * 4, (int)(k >> 32));
-        const uint32_t lo = (uint32_t)__builtin_amdgcn_ds_permute(rank * 4, (int)(uint32_t)k);
-        key = (u64)hi << 32 | lo;
-        close(topk);
-    }
+    u64 key = 0;   // this lane's
+    u64 last = 0;  // the topk-th
     // one more key a lane (0: none)
     __device__ __forceinline__ void offer(u64 k, int topk) {
         u64 in = __ballot(k > last);
@@ -134,7 +115,7 @@ struct TopList {
                            (uint32_t)__builtin_amdgcn_update_dpp(-1, (int)(uint32_t)key, 0x138, 0xF, 0xF, false);
             // (up: the key of the lane below, all ones in lane 0)
             key = key > nk ? key : up > nk ? nk : up;
-            close(topk);
+            last = lane_key(key, topk - 1);
             in &= ~(1ull << src);
             in &= __ballot(k > last);
         }
@@ -144,8 +125,14 @@ struct TopList {
 // ---------------------------------------------------------------------------
 // Rows with many classes: NW waves share a row (or one of the parts it is
 // split into), or with NW = 1 each wave of four has a row of its own.  A lane
-// takes 16-byte vectors, U of them in flight, and keeps its own (m, s, t);
-// scores enter the list of alternatives where they pass its last one.
+// takes 16-byte vectors, LU of them in flight, and keeps its own (m, s, t).
+//
+// The alternatives come from the lanes' maxima, which the sums keep anyway: of 64
+// groups of lanes the topk-th largest maximum is a score that at least topk
+// classes reach, so they all lie in lanes whose own maximum does.  Few do (24 of
+// 1024 for 20 alternatives of random scores); their vectors are read again, and
+// the scores that reach the bound sorted into a list.  The pass over the row costs
+// what it does without alternatives.
 // ---------------------------------------------------------------------------
 constexpr int LU = 4;
 
@@ -155,6 +142,18 @@ struct Part {  // results of a part of a row in the workspace, followed by topk 
     float m, s, t, unused;
 };
 __host__ __device__ inline long long part_bytes(int topk) { return 16 + 8LL * topk; }
+
+// The k-th largest of the lanes' values.
+__device__ __forceinline__ float kth_of_lanes(float m, int k) {
+    int rank = 0;
+#pragma unroll 16
+    for (int l = 0; l < 64; ++l) {
+        const float o = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(m), l));
+        rank += o > m || (o == m && l < lane_id()) ? 1 : 0;
+    }
+    const int at = __ffsll((unsigned long long)__ballot(rank == k - 1)) - 1;
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(m), at));
+}
 
 template <typename T, bool ENT>
 __device__ __forceinline__ void add_vectors(Acc& a, const float (&f)[LU][LV<T>], const float (&vm)[LU]) {
@@ -180,6 +179,9 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void k_logp_rows(LogpArgs 
     constexpr int V = LV<T>, THREADS = NW == 1 ? 256 : NW * 64;
     __shared__ float s_acc[3][NW];
     __shared__ u64 s_key[TOP && NW > 1 ? NW * 64 : 1];
+    __shared__ float s_max[TOP && NW > 1 ? NW * 64 : 1];
+    __shared__ float s_bound;
+    __shared__ int s_n, s_nan;
     const int lane = lane_id(), wid = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int wave = NW == 1 ? 0 : wid;
     const long long item = NW == 1 ? (long long)blockIdx.x * 4 + wid : (long long)blockIdx.x;
@@ -195,18 +197,9 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void k_logp_rows(LogpArgs 
     const T* zv = z + head;
 
     Acc acc = nothing();
-    TopList top;
-    bool begun = false;
-    if (TOP) {
-        top.key = 0;
-        top.close(a.topk);
-    }
-    auto one = [&](int j, bool in) {  // a single score a lane
-        const float f = in ? to_f32(z[j]) : -INFINITY;
-        add(acc, f);
-        if (TOP) top.offer(in ? key_of(f, j) : 0, a.topk);
-    };
-    if (part == 0 && wave == 0 && head) one(lane, lane < head);
+    const bool first = part == 0 && wave == 0 && head, final_ = part == parts - 1 && wave == NW - 1 && tail < a.C;
+    const bool in_h = lane < head, in_t = tail + lane < a.C;
+    const float fh = first && in_h ? to_f32(z[lane]) : -INFINITY, ft = final_ && in_t ? to_f32(z[tail + lane]) : -INFINITY;
 
     typename RawT<16>::type cur[LU], nxt[LU];
     constexpr int STEP = NW * 64 * LU;
@@ -217,9 +210,9 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void k_logp_rows(LogpArgs 
             if (v < v1) to[u] = ld_nt16(zv + (long long)v * V);
         }
     };
-    int base = v0 + wave * (64 * LU);
-    if (base < v1) load(cur, base);
-    for (; base < v1; base += STEP) {
+    const int begin = v0 + wave * (64 * LU);
+    if (begin < v1) load(cur, begin);
+    for (int base = begin; base < v1; base += STEP) {
         if (base + STEP < v1) load(nxt, base + STEP);
         float f[LU][V], vm[LU];
 #pragma unroll
@@ -234,37 +227,63 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void k_logp_rows(LogpArgs 
             for (int i = 1; i < V; ++i) vm[u] = fmaxf(vm[u], f[u][i]);
         }
         add_vectors<T, ENT>(acc, f, vm);
-        if (TOP) {
-            const bool nan = acc.s != acc.s;  // then vm says nothing
-#pragma unroll
-            for (int u = 0; u < LU; ++u) {
-                const int v = base + u * 64 + lane;
-                const bool in = v < v1;
-                const int j = head + v * V;
-                if (__ballot(!(vm[u] <= top.cut) || nan) == 0) continue;
-                u64 own = 0;
-                if (!begun) {  // the list starts as the largest of every lane
-#pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        const u64 k = key_of(f[u][i], j + i);
-                        own = in && k > own ? k : own;
-                    }
-                    if (__ballot(top.key != 0) == 0) top.start(own, a.topk);
-                    else top.offer(own, a.topk);
-                    begun = true;
-                }
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    if (__ballot(!(f[u][i] < top.cut)) == 0) continue;
-                    const u64 k = key_of(f[u][i], j + i);
-                    top.offer(in && k != own ? k : 0, a.topk);
-                }
-            }
-        }
 #pragma unroll
         for (int u = 0; u < LU; ++u) cur[u] = nxt[u];
     }
-    if (part == parts - 1 && wave == NW - 1 && tail < a.C) one(tail + lane, tail + lane < a.C);
+    const float mine = acc.m;
+    if (first) add(acc, fh);
+    if (final_) add(acc, ft);
+
+    TopList top;
+    if (TOP) {
+        bool nan = __ballot(acc.s != acc.s) != 0;  // then the maxima say nothing
+        float bound;
+        if (NW > 1) {
+            s_max[wave * 64 + lane] = mine;
+            if (threadIdx.x == 0) s_n = s_nan = 0;
+            __syncthreads();
+            if (nan && lane == 0) s_nan = 1;
+            if (wave == 0) {
+                float m = mine;
+                for (int w = 1; w < NW; ++w) m = fmaxf(m, s_max[w * 64 + lane]);
+                m = kth_of_lanes(m, a.topk);
+                if (lane == 0) s_bound = m;
+            }
+            __syncthreads();
+            nan = s_nan != 0;
+            bound = s_bound;
+        } else {
+            bound = kth_of_lanes(mine, a.topk);
+        }
+        // (a maximum of LOWEST may be that of nothing, or of -inf alone)
+        const bool all = nan || bound <= LOWEST;
+        if (all) bound = -INFINITY;
+        if (first) top.offer(in_h ? key_of(fh, lane) : 0, a.topk);
+        if (final_) top.offer(in_t ? key_of(ft, tail + lane) : 0, a.topk);
+        const u64 lanes = all ? ~0ull : (u64)__ballot(mine >= bound);
+        const int count = __popcll(lanes);
+        // lane i: the i-th of these lanes
+        const int below = __builtin_amdgcn_mbcnt_hi((uint32_t)(lanes >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)lanes, 0u));
+        const int which = __builtin_amdgcn_ds_permute((lanes >> lane & 1 ? below : count + lane - below) * 4, lane);
+        const int nt = (v1 - v0 + STEP - 1) / STEP * LU;  // vectors of a lane, at most
+        const int together = nt >= 64 ? 1 : 64 / max(nt, 1);  // lanes whose vectors the wave reads at once
+        for (int c0 = 0; c0 < count; c0 += together)
+            for (int t0 = 0; t0 < nt; t0 += 64) {
+                const int ci = c0 + (together > 1 ? lane / nt : 0), t = together > 1 ? lane % nt : t0 + lane;
+                const int of = __shfl(which, min(ci, 63), 64);
+                const int v = begin + t / LU * STEP + t % LU * 64 + of;
+                const bool in = ci < min(count, c0 + together) && t < nt && v < v1;
+                Vec<T, V> q;
+                q.raw = uint4{0u, 0u, 0u, 0u};
+                if (in) q.raw = *reinterpret_cast<const uint4*>(zv + (long long)v * V);
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const float f = to_f32(q.e[i]);
+                    const bool take = in && !(f < bound);
+                    if (__ballot(take)) top.offer(take ? key_of(f, head + v * V + i) : 0, a.topk);
+                }
+            }
+    }
 
     acc = wave_join(acc);
     if (NW > 1) {
@@ -273,7 +292,13 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void k_logp_rows(LogpArgs 
             s_acc[1][wave] = acc.s;
             s_acc[2][wave] = acc.t;
         }
-        if (TOP && lane < a.topk) s_key[wave * a.topk + lane] = top.key;
+        if (TOP) {  // the lists one behind the other, in any order
+            const int have = __popcll(__ballot(lane < a.topk && top.key != 0));
+            int at = 0;
+            if (lane == 0 && have) at = atomicAdd(&s_n, have);
+            at = __builtin_amdgcn_readfirstlane(at);
+            if (lane < have) s_key[at + lane] = top.key;
+        }
         __syncthreads();
         acc = Acc{s_acc[0][0], s_acc[1][0], s_acc[2][0]};
         for (int w = 1; w < NW; ++w) join(acc, Acc{s_acc[0][w], s_acc[1][w], s_acc[2][w]});
@@ -293,19 +318,16 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void k_logp_rows(LogpArgs 
         if (NW == 1) {
             if (lane < a.topk) alternative(lane, top.key);
         } else {  // the waves' lists: a key's place is the number of larger ones
-            const int n = NW * a.topk;
+            const int n = s_n;
             for (int i = tid; i < n; i += THREADS) {
                 const u64 k = s_key[i];
                 int rank = 0;
+#pragma unroll 8
                 for (int o = 0; o < n; ++o) rank += s_key[o] > k ? 1 : 0;
-                // (a part of fewer classes than topk has keys 0, all behind)
-                if (k ? rank < a.topk : false) alternative(rank, k);
+                if (rank < a.topk) alternative(rank, k);
             }
-            if (out) {
-                int have = 0;
-                for (int o = 0; o < n; ++o) have += s_key[o] != 0 ? 1 : 0;
-                for (int i = have + tid; i < a.topk; i += THREADS) alternative(i, 0);
-            }
+            // (a part may have fewer classes than topk: keys 0)
+            for (int i = n + tid; i < a.topk; i += THREADS) alternative(i, 0);
         }
     }
     if (tid != 0) return;
