@@ -1,0 +1,154 @@
+"""Host-only checks of the log probabilities and the orthogonalised updates: the
+C ABI refuses bad arguments before anything reaches the GPU, the workspace
+queries answer, and the binding reads layouts and strides as documented."""
+from __future__ import annotations
+
+import ctypes
+import os
+
+import pytest
+import torch
+
+b = pytest.importorskip("paper_2011_12025_amd._binding")
+import paper_2011_12025_amd as sb  # noqa: E402
+
+
+def at(i):
+    return ctypes.c_void_p(0x100000000 * (i + 1))  # never dereferenced
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(b.LIB_PATH):
+        pytest.fail("libsegblocks.so is not built (run __graft_entry__.build())")
+    return b.lib()
+
+
+def scores(lib, **kw):
+    a = dict(z=at(0), dtype=1, layout=1, N=4, C=19, H=8, W=8, C_buf=24, labels=at(1), ignore=255, topk=2, logp=at(2),
+             lse=at(3), entropy=at(4), tl=at(5), ti=at(6), ws=None, n=0)
+    a.update(kw)
+    return lib.segblocks_log_probs(a["z"], a["dtype"], a["layout"], a["N"], a["C"], a["H"], a["W"], a["C_buf"], a["labels"],
+                                   a["ignore"], a["topk"], a["logp"], a["lse"], a["entropy"], a["tl"], a["ti"], a["ws"],
+                                   a["n"], None)
+
+
+@pytest.mark.parametrize("kw,code,msg", [
+    (dict(dtype=3), -1, "dtype"), (dict(layout=2), -1, "layout"), (dict(N=0), -1, "positive"), (dict(C=0), -1, "positive"),
+    (dict(C=25), -1, "hold the classes"), (dict(topk=-1), -1, "topk"), (dict(topk=20), -1, "topk"),
+    (dict(C=100, C_buf=100, topk=65), -1, "topk"), (dict(z=None), -1, "NULL"), (dict(lse=None), -1, "NULL"),
+    (dict(logp=None), -1, "together"), (dict(labels=None), -1, "together"), (dict(tl=None), -1, "topk > 0"),
+    (dict(topk=0), -1, "topk > 0"), (dict(lse=at(2)), -1, "overlap"), (dict(tl=at(0)), -1, "overlap"),
+    (dict(N=1 << 20, H=1 << 10, W=1 << 10), -2, "too large"), (dict(C=1 << 30 | 1, C_buf=1 << 30 | 1), -2, "2^30"),
+    (dict(N=1, C=131072, C_buf=131072, H=1, W=1), -4, "workspace"),
+    (dict(N=1, C=131072, C_buf=131072, H=1, W=1, ws=ctypes.c_void_p(0x900000010), n=1 << 20), -1, "aligned"),
+    (dict(N=1, C=131072, C_buf=131072, H=1, W=1, ws=at(3), n=1 << 20), -1, "workspace overlaps"),
+])
+def test_log_probs_refuses(lib, kw, code, msg):
+    assert scores(lib, **kw) == code
+    assert msg in lib.segblocks_last_error().decode()
+
+
+def grad(lib, **kw):
+    a = dict(z=at(0), dtype=1, layout=1, N=4, C=19, H=8, W=8, C_buf=24, labels=at(1), ignore=255, lse=at(2), d_logp=at(3),
+             entropy=at(4), d_entropy=at(5), topk=2, ti=at(6), d_top=at(7), C_dbuf=19, dz=at(8))
+    a.update(kw)
+    return lib.segblocks_log_probs_backward(a["z"], a["dtype"], a["layout"], a["N"], a["C"], a["H"], a["W"], a["C_buf"],
+                                            a["labels"], a["ignore"], a["lse"], a["d_logp"], a["entropy"], a["d_entropy"],
+                                            a["topk"], a["ti"], a["d_top"], a["C_dbuf"], a["dz"], None)
+
+
+@pytest.mark.parametrize("kw,code,msg", [
+    (dict(dtype=-1), -1, "dtype"), (dict(C_dbuf=18), -1, "hold the classes"), (dict(dz=None), -1, "NULL"),
+    (dict(lse=None), -1, "NULL"), (dict(labels=None), -1, "needs labels"), (dict(entropy=None), -1, "needs entropy"),
+    (dict(d_top=None), -1, "topk > 0"), (dict(topk=0), -1, "topk > 0"), (dict(dz=at(0)), -1, "overlaps"),
+    (dict(dz=at(7)), -1, "overlaps"), (dict(d_logp=None, d_entropy=None, topk=0, ti=None, d_top=None), -1, "no gradient"),
+])
+def test_log_probs_backward_refuses(lib, kw, code, msg):
+    assert grad(lib, **kw) == code
+    assert msg in lib.segblocks_last_error().decode()
+
+
+def orth(lib, steps=5, coef=None, eps=1e-7, dtype=1, count=1, ws=at(20), n=1 << 40, **kw):
+    m = b.Matrix(at(0).value, at(1).value, 1, 64, 576, 576, 576, 0, 0)
+    for k, v in kw.items():
+        setattr(m, k, v.value if isinstance(v, ctypes.c_void_p) else v)
+    c = (ctypes.c_double * (3 * max(steps, 1)))(*(coef or [3.4445, -4.775, 2.0315]) * max(steps, 1))
+    return lib.segblocks_orthogonalize(ctypes.pointer(m) if count else None, count, dtype, steps, c, eps, ws, n, None)
+
+
+@pytest.mark.parametrize("kw,code,msg", [
+    (dict(dtype=5), -1, "dtype"), (dict(count=0), -1, "matrices"), (dict(count=5000), -1, "4096"),
+    (dict(rows=0), -1, "positive"), (dict(batch=-1), -1, "positive"), (dict(ld=500), -1, "overlap"),
+    (dict(ld_out=1), -1, "overlap"), (dict(rows=40000, cols=40000, ld=40000, ld_out=40000), -2, "too large"),
+    (dict(batch=2, batch_stride=1 << 20, batch_stride_out=100), -1, "strides"), (dict(batch=2, batch_stride=-4), -1, "strides"),
+    (dict(steps=0), -1, "steps"), (dict(steps=33), -1, "steps"), (dict(coef=[float("nan"), 0, 0]), -1, "coefficient"),
+    (dict(coef=[1e9, 0, 0]), -1, "coefficient"), (dict(eps=-1.0), -1, "eps"), (dict(eps=float("nan")), -1, "eps"),
+    (dict(update=None), -1, "NULL"), (dict(out=None), -1, "NULL"), (dict(out=at(0)), -1, "overlap"),
+    (dict(ws=None), -4, "workspace"), (dict(n=4096), -4, "workspace"), (dict(ws=at(1)), -1, "overlap"),
+    (dict(ws=ctypes.c_void_p(0x900000010)), -1, "aligned"),
+])
+def test_orthogonalize_refuses(lib, kw, code, msg):
+    assert orth(lib, **kw) == code
+    assert msg in lib.segblocks_last_error().decode()
+
+
+def test_workspace_queries():
+    bf = torch.bfloat16
+    assert sb.log_probs_workspace_size(bf, b.SB_NHWC, 4096, 50000, 1, 1, 50000, 5) == 0
+    assert sb.log_probs_workspace_size(bf, b.SB_NHWC, 1, 131072, 1, 1, 131072, 5) > 0
+    with pytest.raises(sb._b.SegBlocksError):
+        sb.log_probs_workspace_size(bf, b.SB_NHWC, 1, 10, 1, 1, 10, 11)
+    one = sb.orthogonalize_workspace_size(torch.empty(64, 576))
+    assert one > 64 * 576 * 8
+    # groups of a long list share the workspace
+    many = sb.orthogonalize_workspace_size([torch.empty(64, 576)] * 300)
+    assert one < many < 60 * one
+
+
+@pytest.mark.parametrize("t,want", [
+    (torch.empty(5, 7), (b.SB_NHWC, 5, 7, 1, 1, 7)), (torch.empty(5, 9)[:, 1:8], (b.SB_NHWC, 5, 7, 1, 1, 9)),
+    (torch.empty(2, 5, 7), (b.SB_NHWC, 10, 7, 1, 1, 7)), (torch.empty(2, 5, 9)[:, :, :7], (b.SB_NHWC, 10, 7, 1, 1, 9)),
+    (torch.empty(2, 5, 9)[:, 4:, :7], (b.SB_NHWC, 2, 7, 1, 1, 45)), (torch.empty(1, 7), (b.SB_NHWC, 1, 7, 1, 1, 7)),
+    (torch.empty(2, 6, 3, 4), (b.SB_NCHW, 2, 6, 3, 4, 6)), (torch.empty(2, 8, 3, 4)[:, :6], (b.SB_NCHW, 2, 6, 3, 4, 8)),
+    (torch.empty(2, 8, 3, 4).contiguous(memory_format=torch.channels_last)[:, 1:7], (b.SB_NHWC, 2, 6, 3, 4, 8)),
+    (torch.empty(2, 6, 1, 1), (b.SB_NHWC, 2, 6, 1, 1, 6)), (torch.empty(2, 8, 1, 1)[:, :6], (b.SB_NHWC, 2, 6, 1, 1, 8)),
+    (torch.empty(1, 8, 3, 4)[:, :6], (b.SB_NCHW, 1, 6, 3, 4, 6)), (torch.empty(2, 1, 3, 4), (b.SB_NHWC, 2, 1, 3, 4, 1)),
+    (torch.empty(0, 7), (b.SB_NHWC, 0, 7, 1, 1, 7)),
+])
+def test_scores_are_read_as_they_lie(t, want):
+    assert sb._scores(t.shape, t.stride()) == want
+
+
+@pytest.mark.parametrize("t", [
+    torch.empty(7, 5).t(), torch.empty(5, 14)[:, ::2], torch.empty(1, 7).expand(5, 7), torch.empty(4, 5, 7)[:, ::2],
+    torch.empty(2, 6, 3, 4).permute(0, 1, 3, 2), torch.empty(2, 6, 3, 8)[..., ::2], torch.empty(2, 6, 3, 4)[:, :, :2],
+    torch.empty(5), torch.empty(1, 1, 1, 1, 1), torch.empty(5, 0),
+])
+def test_scores_that_are_refused(t):
+    with pytest.raises(ValueError):
+        sb._scores(t.shape, t.stride())
+
+
+def test_updates_are_read_as_they_lie():
+    m = torch.empty(6, 10)
+    assert sb._matrix(m) == (1, 6, 10, 10, 0)
+    assert sb._matrix(m.t()) == (1, 6, 10, 10, 0)  # taken transposed
+    assert sb._matrix(m[1:5, 2:9]) == (1, 4, 7, 10, 0)
+    assert sb._matrix(m[::2]) == (1, 3, 10, 20, 0)
+    assert sb._matrix(m[:, :1]) == (1, 6, 1, 10, 0)
+    assert sb._matrix(torch.empty(3, 6, 10)[:, :4]) == (3, 4, 10, 10, 60)
+    assert sb._matrix(torch.empty(4, 5, 3, 3)) == (1, 4, 45, 45, 0)
+    assert sb._matrix(torch.empty(4, 5, 3, 3).contiguous(memory_format=torch.channels_last)) == (1, 4, 45, 45, 0)
+    for bad in (m[:, ::2], torch.empty(5), m[:1].expand(4, 10), torch.empty(4, 5, 3, 3)[:, :3]):
+        with pytest.raises(ValueError):
+            sb._matrix(bad)
+
+
+def test_cpu_tensors_are_refused():
+    with pytest.raises(ValueError, match="cuda"):
+        sb.log_probs(torch.empty(2, 5))
+    with pytest.raises(ValueError, match="cuda"):
+        sb.log_probs_backward(torch.empty(2, 5), None, torch.empty(2))
+    with pytest.raises(ValueError, match="cuda"):
+        sb.orthogonalize(torch.empty(2, 5))
