@@ -65,9 +65,11 @@ constexpr int MAXP = 1024;  // workgroups that make X, each with its sum of squa
 constexpr int MAXA = 1024;  // workgroups that look for the largest value
 constexpr long long W_SUM = 4 * MAXA, W_X = W_SUM + 4 * MAXP;  // [0]: the largest values
 __host__ __device__ inline long long w_x_bytes(int sp, int Lp) { return (long long)sp * Lp * 4; }
-__host__ __device__ inline long long w_xt(int sp, int Lp, int i) { return W_X + (1 + i) * w_x_bytes(sp, Lp); }
+// X and its transpose, each twice: a block's and the next one's
+__host__ __device__ inline long long w_x(int sp, int Lp, int i) { return W_X + i * w_x_bytes(sp, Lp); }
+__host__ __device__ inline long long w_xt(int sp, int Lp, int i) { return W_X + (2 + i) * w_x_bytes(sp, Lp); }
 __host__ __device__ inline long long w_sym(int sp, int Lp, int i) {
-    return W_X + 3 * w_x_bytes(sp, Lp) + i * ((long long)sp * sp * 4);
+    return W_X + 4 * w_x_bytes(sp, Lp) + i * ((long long)sp * sp * 4);
 }
 constexpr int SYMS = 5;  // A, T and three that P and Q take in turn
 
@@ -228,7 +230,7 @@ __global__ __launch_bounds__(WG) void k_orth_prep(Table tb) {
     const int e = scale_of(q, ws), tid = (int)threadIdx.x;
     const bool tall = q.m > q.n;
     const int mp = tall ? q.Lp : q.sp, np = tall ? q.sp : q.Lp, tn = np / 64, tiles = (mp / 64) * tn, wgs = prep_wgs(q);
-    char* X = ws + W_X;                     // [sp][Lp]
+    char* X = ws + w_x(q.sp, q.Lp, 0);      // [sp][Lp]
     char* Xt = ws + w_xt(q.sp, q.Lp, 0);    // [Lp][sp]
     float sum = 0.0f;
     for (int t = p.t; t < tiles; t += wgs) {
@@ -322,13 +324,14 @@ __device__ __forceinline__ void dma16(const char* from, unsigned char* to) {
     __builtin_amdgcn_global_load_lds(from, (lds_ptr)to, 16, 0, 0);
 }
 
-// rows of A and B from their first element on; the tile ends in LDS as fp32.
+// rows of A and B from their first element on; the tile ends in LDS as fp32.  NA,
+// NB: numbers of an element that take part, SA, SB: that are stored (1 of 2: hi).
 //
 // A wave's DMA instructions are spread over its MFMAs: a CU takes one (1 KB) in
 // about 28 cycles, and a wave that issues a stage's eight in a row stands still
 // until the last is taken (4096^2 x 4096: loads alone 100 us, MFMAs alone 112, one
 // after the other 207).
-template <int T, int NA, int NB>
+template <int T, int NA, int NB, int SA = NA, int SB_ = NB>
 __device__ __forceinline__ void product_tile(const char* A, long long pa, const char* B, long long pb, int step0,
                                              int steps, unsigned char* lds) {
     constexpr int SB = stage_bytes<T, NA, NB>(), HB = T * 64 * (NA + NB), OB = T * 64 * NA, NST = stages<T, NA, NB>();
@@ -351,8 +354,8 @@ __device__ __forceinline__ void product_tile(const char* A, long long pa, const 
         from[i] = (unsigned)(r * (i < LA ? pa : pb) + chunk * 16);
     }
     auto dma = [&](int i, int s, int buf) {  // instruction i of stage s
-        const int k = i / LH * GROUPS + group, j = i % LH, np = j < LA ? NA : NB;
-        const char* base = (j < LA ? A : B) + ((long long)(step0 + s) * KS<T> + k) * (64 * np);
+        const int k = i / LH * GROUPS + group, j = i % LH;
+        const char* base = (j < LA ? A : B) + ((long long)(step0 + s) * KS<T> + k) * (64 * (j < LA ? SA : SB_));
         unsigned char* to = lds + buf * SB + k * HB + (j < LA ? j : j - LA) * (WG * 16) + (j < LA ? 0 : OB) + wave * 1024;
         dma16(base + from[j], to);
     };
@@ -463,7 +466,7 @@ __device__ __forceinline__ void sym_tile(int t, int n, int& bi, int& bj) {
 // matrices [sp][sp], and their mirror image.
 template <int T, int R>
 __device__ __forceinline__ void store_sym(float* C, char* out, const char* D, int sp, int r0, int c0, bool mirror,
-                                          float alpha, float beta, float gamma) {
+                                          bool one, float alpha, float beta, float gamma) {
     for (int e = (int)threadIdx.x; e < R * T / 8; e += NT<T>) {
         const int r = e / (T / 8), k = (e % (T / 8)) * 8, K = c0 + k;
         const long long row = (long long)(r0 + r) * sp * 4;
@@ -477,6 +480,9 @@ __device__ __forceinline__ void store_sym(float* C, char* out, const char* D, in
             for (int i = 0; i < 8; ++i)
                 v[i] += beta * ((float)hi.e[i] + (float)lo.e[i]) + (r0 + r == K + i ? gamma : 0.0f);
         }
+        if (one)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = (float)(f16)v[i];
         store8<2>(out + row, K, v);
 #pragma unroll
         for (int i = 0; i < 8; ++i) C[r * CP<T> + k + i] = v[i];
@@ -501,7 +507,9 @@ struct SymLaunch {
     SymJob job[2];
     int tiles;  // of one product
     int whole, parts, first;
+    int x;      // of X X^T: which X
     int leave;  // sums of every tile, for k_orth_steps
+    int one;    // the result rounded to one fp16 number (its lo is 0)
     float eps;
     float* sums;  // [unit][T * T], units counted from the first split tile's (whole < 0: from the first of all)
 };
@@ -537,11 +545,11 @@ __device__ __forceinline__ void sym_out(const OMat& q, char* ws, const SymLaunch
         const float f = norm_factor(q, ws, s.eps);
         alpha *= f * f;
     }
-    store_sym<T, R>(C, sym(j.c), GRAM || j.d < 0 ? nullptr : sym(j.d), q.sp, bi * T + part * R, bj * T, bi != bj, alpha,
-                    j.beta, j.gamma);
+    store_sym<T, R>(C, sym(j.c), GRAM || j.d < 0 ? nullptr : sym(j.d), q.sp, bi * T + part * R, bj * T, bi != bj,
+                    s.one, alpha, j.beta, j.gamma);
 }
 
-template <int T, int NP, bool GRAM>
+template <int T, int NP, int S, bool GRAM>  // NP of the S stored numbers of an element
 __global__ __launch_bounds__(NT<T>, 2) void k_orth_sym(Table tb, SymLaunch s) {
     extern __shared__ __align__(16) unsigned char lds[];
     const SymUnit u = sym_unit<T>(tb, s, (int)blockIdx.x);
@@ -552,10 +560,10 @@ __global__ __launch_bounds__(NT<T>, 2) void k_orth_sym(Table tb, SymLaunch s) {
     sym_tile(u.p.t, q.sp / T, bi, bj);
     const int K = GRAM ? q.Lp : q.sp, steps = K / step_k<T>();
     const int k0 = (int)((long long)steps * u.part / u.parts), k1 = (int)((long long)steps * (u.part + 1) / u.parts);
-    const long long pitch = (long long)K * (2 * NP);
-    const char* A = GRAM ? ws + W_X : ws + w_sym(q.sp, q.Lp, j.a);
+    const long long pitch = (long long)K * (2 * S);
+    const char* A = GRAM ? ws + w_x(q.sp, q.Lp, s.x) : ws + w_sym(q.sp, q.Lp, j.a);
     const char* B = GRAM ? A : ws + w_sym(q.sp, q.Lp, j.b);
-    product_tile<T, NP, NP>(A + bi * T * pitch, pitch, B + bj * T * pitch, pitch, k0, k1 - k0, lds);
+    product_tile<T, NP, NP, S, S>(A + bi * T * pitch, pitch, B + bj * T * pitch, pitch, k0, k1 - k0, lds);
     float* C = (float*)lds;
     if (u.parts > 1 || s.leave) {
         float4* out = (float4*)(s.sums + u.unit * (T * T));
@@ -736,23 +744,55 @@ __global__ __launch_bounds__(512) void k_orth_steps(Table tb, Steps st) {
     }
 }
 
-// Q X: the next block's X and its transpose, or the result.
-template <int T, int NP, typename TO, bool LAST>
-__global__ __launch_bounds__(NT<T>, 2) void k_orth_apply(Table tb, int Q, int xt, float alpha, float eps, int first) {
+// Q X: the next block's X and its transpose, or the result.  DIRECT: the single
+// step a X + B X instead, Q being B, where both factors of the product are their
+// hi alone and a X has what X has.  S: stored numbers of an element of X.
+struct Apply {
+    int Q, xt, first;
+    float alpha, a, eps;  // alpha Q X + a X
+};
+template <int T, int S, typename TO, bool LAST, bool DIRECT>
+__global__ __launch_bounds__(NT<T>, 2) void k_orth_apply(Table tb, Apply ap) {
     extern __shared__ __align__(16) unsigned char lds[];
+    constexpr int NQ = DIRECT ? 1 : 2, NX = DIRECT ? 1 : S;
     const Place p = place(tb, [](const OMat& q) { return (q.sp / T) * (q.Lp / T); }, (int)blockIdx.x);
     const OMat& q = tb.mat[p.mat];
     char* ws = q.ws + p.b * q.ws_one;
     // strips of eight rows of Q, each along L
     const int strip = p.t / (8 * (q.Lp / T)), h = min(8, q.sp / T - 8 * strip), local = p.t - strip * (8 * (q.Lp / T));
     const int k = local / h, i = 8 * strip + (local - k * h);
-    const char* qm = ws + w_sym(q.sp, q.Lp, Q) + (long long)i * T * q.sp * 4;
-    const char* xm = ws + w_xt(q.sp, q.Lp, xt) + (long long)k * T * q.sp * (2 * NP);
+    const long long pq = (long long)q.sp * 4, px = (long long)q.sp * (2 * S);
+    const char* X = ws + w_x(q.sp, q.Lp, ap.xt);
+    const char* Xt = ws + w_xt(q.sp, q.Lp, ap.xt);
+    const char* qm = ws + w_sym(q.sp, q.Lp, ap.Q) + i * T * pq;
+    const char* xm = Xt + k * T * px;
     const bool tall = LAST && q.m > q.n;  // then the tile's rows are those of Xt
-    if (tall) product_tile<T, NP, 2>(xm, (long long)q.sp * (2 * NP), qm, (long long)q.sp * 4, 0, q.sp / step_k<T>(), lds);
-    else product_tile<T, 2, NP>(qm, (long long)q.sp * 4, xm, (long long)q.sp * (2 * NP), 0, q.sp / step_k<T>(), lds);
+    if (tall) product_tile<T, NX, NQ, S, 2>(xm, px, qm, pq, 0, q.sp / step_k<T>(), lds);
+    else product_tile<T, NQ, NX, 2, S>(qm, pq, xm, px, 0, q.sp / step_k<T>(), lds);
     float* C = (float*)lds;
-    const float f = alpha * (first ? norm_factor(q, ws, eps) : 1.0f);
+    const float f = ap.first ? norm_factor(q, ws, ap.eps) : 1.0f;
+    {  // each thread its own eights
+        const float alpha = f * ap.alpha, a = f * ap.a;
+        const char* D = tall ? Xt : X;
+        const int r0 = (tall ? k : i) * T, c0 = (tall ? i : k) * T;
+        const long long pd = (long long)(tall ? q.sp : q.Lp) * (2 * S);
+        for (int e = (int)threadIdx.x; e < T * T / 8; e += NT<T>) {
+            const int r = e / (T / 8), c = (e % (T / 8)) * 8;
+            float* v = C + r * CP<T> + c;
+            if constexpr (DIRECT) {
+                const char* d = D + (r0 + r) * pd + at_k<S>(c0 + c);
+                const Vec<f16, 8> hi = vload<f16, 8>((const f16*)d);
+                Vec<f16, 8> lo = vzero<f16, 8>();
+                if (S == 2) lo = vload<f16, 8>((const f16*)(d + 64));
+#pragma unroll
+                for (int x = 0; x < 8; ++x) v[x] = alpha * v[x] + a * ((float)hi.e[x] + (float)lo.e[x]);
+            } else {
+#pragma unroll
+                for (int x = 0; x < 8; ++x) v[x] *= alpha;
+            }
+        }
+        __syncthreads();
+    }
     if constexpr (LAST) {
         TO* o = (TO*)q.o + p.b * q.bstride_o;
         const int r0 = (tall ? k : i) * T, c0 = (tall ? i : k) * T;
@@ -761,19 +801,17 @@ __global__ __launch_bounds__(NT<T>, 2) void k_orth_apply(Table tb, int Q, int xt
             const int x = e / (T / V), y = e % (T / V) * V, r = r0 + x, c = c0 + y;
             Vec<TO, V> v;
 #pragma unroll
-            for (int i = 0; i < V; ++i) v.e[i] = from_f32<TO>(f * C[x * CP<T> + y + i]);
+            for (int n = 0; n < V; ++n) v.e[n] = from_f32<TO>(C[x * CP<T> + y + n]);
             if (r >= q.m) continue;
             TO* to = o + r * q.ld_o + c;
             if ((q.vec & 2) && c + V <= q.n) *reinterpret_cast<uint4*>(to) = v.raw;
             else
-                for (int i = 0; i < V; ++i)
-                    if (c + i < q.n) to[i] = v.e[i];
+                for (int n = 0; n < V; ++n)
+                    if (c + n < q.n) to[n] = v.e[n];
         }
     } else {
-        for (int e = (int)threadIdx.x; e < T * T; e += NT<T>) C[e / T * CP<T> + e % T] *= f;
-        __syncthreads();
-        store_tile<T, 2, false>(C, ws + W_X, q.Lp, i * T, k * T);
-        store_tile<T, 2, true>(C, ws + w_xt(q.sp, q.Lp, xt ^ 1), q.sp, k * T, i * T);
+        store_tile<T, 2, false>(C, ws + w_x(q.sp, q.Lp, ap.xt ^ 1), q.Lp, i * T, k * T);
+        store_tile<T, 2, true>(C, ws + w_xt(q.sp, q.Lp, ap.xt ^ 1), q.sp, k * T, i * T);
     }
 }
 
@@ -936,7 +974,7 @@ struct Runner {
         err = hipGetLastError();
     }
 
-    template <int TILE, int P, bool GRAM>
+    template <int TILE, int P, int S, bool GRAM>
     void sym_t(SymLaunch& s, int jobs) {
         constexpr int lds = product_lds<TILE, P, P>(), SLICES = TILE / JOIN_ROWS<TILE>;
         auto tiles = [](const OMat& q) { const int t = q.sp / TILE; return t * (t + 1) / 2; };
@@ -957,7 +995,7 @@ struct Runner {
                 unit += tiles(q) * q.batch * q.parts;
             }
             s.whole = -1;
-            run<NT<TILE>>(k_orth_sym<TILE, P, GRAM>, number(tb, [&](const OMat& q) { return tiles(q) * q.parts; }), lds, s);
+            run<NT<TILE>>(k_orth_sym<TILE, P, S, GRAM>, number(tb, [&](const OMat& q) { return tiles(q) * q.parts; }), lds, s);
             if (!s.leave)
                 run<NT<TILE>>(k_orth_join<TILE, GRAM>,
                               number(tb, [&](const OMat& q) { return q.parts > 1 ? tiles(q) * SLICES : 0; }), 0, s);
@@ -967,33 +1005,80 @@ struct Runner {
         s.whole = c.whole;
         s.parts = c.parts;
         const int rest = s.tiles * jobs - c.whole;
-        run<NT<TILE>>(k_orth_sym<TILE, P, GRAM>, (unsigned)(c.whole + rest * c.parts), lds, s);
+        run<NT<TILE>>(k_orth_sym<TILE, P, S, GRAM>, (unsigned)(c.whole + rest * c.parts), lds, s);
         if (rest) run<NT<TILE>>(k_orth_join<TILE, GRAM>, (unsigned)(rest * SLICES), 0, s);
     }
-    template <int P, bool GRAM>
-    void sym(SymLaunch s, int jobs) {
-        if (tile_of(sym_count(tb, 128) * jobs, wide) == 128) sym_t<128, P, GRAM>(s, jobs);
-        else sym_t<64, P, GRAM>(s, jobs);
+    template <int P, int S, bool GRAM>
+    void sym(SymLaunch s, int jobs = 1) {
+        if (tile_of(sym_count(tb, 128) * jobs, wide) == 128) sym_t<128, P, S, GRAM>(s, jobs);
+        else sym_t<64, P, S, GRAM>(s, jobs);
     }
-    void products(const SymJob& a) { sym<2, false>(SymLaunch{{a, a}}, 1); }
-    void products(const SymJob& a, const SymJob& b) { sym<2, false>(SymLaunch{{a, b}}, 2); }
+    void products(const SymJob& a) { sym<2, 2, false>(SymLaunch{{a, a}}); }
+    void products(const SymJob& a, const SymJob& b) { sym<2, 2, false>(SymLaunch{{a, b}}, 2); }
 
-    template <int TILE, int P, bool LAST>
-    void apply_t(int Q, int xt, float alpha, int first) {
-        run<NT<TILE>>(k_orth_apply<TILE, P, T, LAST>, number(tb, [](const OMat& q) { return (q.sp / TILE) * (q.Lp / TILE); }),
-            product_lds<TILE, 2, P>(), Q, xt, alpha, eps, first);
+    template <int TILE, int S, bool LAST, bool DIRECT>
+    void apply_t(const Apply& ap) {
+        run<NT<TILE>>(k_orth_apply<TILE, S, T, LAST, DIRECT>,
+                      number(tb, [](const OMat& q) { return (q.sp / TILE) * (q.Lp / TILE); }),
+                      product_lds<TILE, DIRECT ? 1 : 2, DIRECT ? 1 : S>(), ap);
     }
-    template <int P, bool LAST>
-    void apply(int Q, int xt, float alpha, int first) {
+    template <int S, bool LAST, bool DIRECT>
+    void apply(const Apply& ap) {
         long long n = 0;
         for (int i = 0; i < tb.count; ++i) n += (long long)(tb.mat[i].sp / 128) * (tb.mat[i].Lp / 128) * tb.mat[i].batch;
-        if (tile_of(n, wide) == 128) apply_t<128, P, LAST>(Q, xt, alpha, first);
-        else apply_t<64, P, LAST>(Q, xt, alpha, first);
+        if (tile_of(n, wide) == 128) apply_t<128, S, LAST, DIRECT>(ap);
+        else apply_t<64, S, LAST, DIRECT>(ap);
+    }
+    template <bool DIRECT>
+    void apply(const Apply& ap, bool last) {
+        if (ap.first) last ? apply<NP, true, DIRECT>(ap) : apply<NP, false, DIRECT>(ap);
+        else last ? apply<2, true, DIRECT>(ap) : apply<2, false, DIRECT>(ap);
+    }
+
+    // One step at a time with products of single fp16 numbers, for bf16 alone (the
+    // head of this file): where it takes fewer of them than blocks do.
+    bool direct(int steps) const {
+        if (!std::is_same<T, bf16>::value || single) return false;
+        double a = 0, b = 0;
+        for (int i = 0; i < tb.count; ++i) {
+            const double s = tb.mat[i].sp, L = tb.mat[i].Lp, n = tb.mat[i].batch;
+            a += n * steps * (3 * s * s * L + s * s * s);
+            b += n * (5 * s * s * L + 3 * std::max(1, 4 * steps - 3) * s * s * s);
+        }
+        return a < b;
+    }
+    hipError_t go_direct(int steps, const double* coef) {
+        double lambda = 1.0;
+        int ex = 0;
+        for (int k = 0; k < steps; ++k) {
+            const double* c = coef + 3 * k;
+            const Bound b = bound_of(c, lambda);
+            const bool last = k + 1 == steps;
+            auto q = [&](double y) { return y > 0.0 && y <= lambda ? fabs(y * (c[1] + y * c[2])) : 0.0; };
+            const double bb = std::max(q(lambda), c[2] != 0.0 ? q(-c[1] / (2.0 * c[2])) : 0.0);
+            const int ea = exponent(lambda), eb = exponent(std::min(std::max(bb, 1e-30), 1e30));
+            const int ex2 = last ? 0 : exponent(sqrt(b.lambda));
+            SymLaunch s{{{0, 0, 0, -1, pow2(ea - 2 * ex), 0.0f, 0.0f}, {}}};
+            s.first = k == 0;
+            s.x = k & 1;
+            s.one = 1;
+            if (k == 0) sym<1, NP, true>(s);
+            else sym<1, 2, true>(s);
+            s = SymLaunch{{{0, 0, 1, 0, (float)(c[2] * pow2(eb - 2 * ea)), (float)(c[1] * pow2(eb - ea)), 0.0f}, {}}};
+            s.one = 1;
+            sym<1, 2, false>(s);
+            apply<true>(Apply{1, k & 1, k == 0, pow2(ex2 - eb - ex), (float)(c[0] * pow2(ex2 - ex)), eps}, last);
+            lambda = b.lambda;
+            ex = ex2;
+        }
+        return err;
     }
 
     hipError_t go(int steps, const double* coef) {
         if (!std::is_same<T, f16>::value) run(k_orth_amax<T>, number(tb, amax_wgs), 0);
         run(k_orth_prep<T>, number(tb, prep_wgs), 0);
+        if constexpr (std::is_same<T, bf16>::value)
+            if (direct(steps)) return go_direct(steps, coef);
         double lambda = 1.0;
         int xt = 0, ex = 0, step = 0;  // X is stored times 2^ex (and 1 / norm_factor in the first block)
         for (bool first = true; step < steps; first = false) {
@@ -1010,9 +1095,10 @@ struct Runner {
             SymLaunch gram{{{0, 0, 0, -1, pow2(ea - 2 * ex), 0.0f, 0.0f}, {}}};
             gram.first = first;
             gram.leave = single;
+            gram.x = xt;
             Steps list{};
-            if (first) sym<NP, true>(gram, 1);
-            else sym<2, true>(gram, 1);
+            if (first) sym<NP, NP, true>(gram);
+            else sym<2, 2, true>(gram);
             int Q = -1, eq = 0;  // Q: which of the workspace's matrices 2, 3, 4
             double qb = 1.0;
             for (int k = 0; k < len; ++k, ++step) {
@@ -1054,15 +1140,8 @@ struct Runner {
                 run<512>(k_orth_steps, number(tb, [](const OMat&) { return 1; }), STEPS_LDS, list);
             }
             const int ex2 = exponent(sqrt(lambda));
-            const float a = pow2((last ? 0 : ex2) - eq - ex);
-            if (last) {
-                if (first) apply<NP, true>(Q, xt, a, 1);
-                else apply<2, true>(Q, xt, a, 0);
-            } else {
-                if (first) apply<NP, false>(Q, xt, a, 1);
-                else apply<2, false>(Q, xt, a, 0);
-                xt ^= 1;
-            }
+            apply<false>(Apply{Q, xt, first, pow2((last ? 0 : ex2) - eq - ex), 0.0f, eps}, last);
+            xt ^= 1;
             ex = ex2;
         }
         return err;
