@@ -329,8 +329,10 @@ __device__ __forceinline__ void dma16(const char* from, unsigned char* to) {
 //
 // A wave's DMA instructions are spread over its MFMAs: a CU takes one (1 KB) in
 // about 28 cycles, and a wave that issues a stage's eight in a row stands still
-// until the last is taken (4096^2 x 4096: loads alone 100 us, MFMAs alone 112, one
-// after the other 207).
+// until the last is taken.  Half of 4096 x 4096 x 4096 in three products: DMA alone
+// 100 us, MFMAs with their LDS reads alone 112, together 207 and spread 196 (1.08
+// PFLOP/s of MFMA, where a large library product reaches 1.21).  More stages (one
+// workgroup of eight waves a CU), or operands read a stage ahead, were no faster.
 template <int T, int NA, int NB, int SA = NA, int SB_ = NB>
 __device__ __forceinline__ void product_tile(const char* A, long long pa, const char* B, long long pb, int step0,
                                              int steps, unsigned char* lds) {
@@ -1038,7 +1040,8 @@ struct Runner {
     // One step at a time with products of single fp16 numbers, for bf16 alone (the
     // head of this file): where it takes fewer of them than blocks do.
     bool direct(int steps) const {
-        if (!std::is_same<T, bf16>::value || single) return false;
+        // (past five steps the slopes of the polynomial near 1 add up these roundings: 2.4e-3 at six)
+        if (!std::is_same<T, bf16>::value || single || steps > 5) return false;
         double a = 0, b = 0;
         for (int i = 0; i < tb.count; ++i) {
             const double s = tb.mat[i].sp, L = tb.mat[i].Lp, n = tb.mat[i].batch;
