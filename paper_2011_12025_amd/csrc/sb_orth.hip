@@ -851,6 +851,8 @@ Cut cut_of(long long n, int most) {
 }
 
 // Tiles of 128 where they give every CU one, else of 64 (and for single tiles).
+// fp32, one matrix, with the border at 100, 256 and 500 tiles: 1500 x 1500 581,
+// 592, 592 us, 2048 x 2048 1025, 936, 1000, 1024 x 4096 374, 371, 414.
 int tile_of(long long n128, bool fits) { return fits && n128 >= 256 ? 128 : 64; }
 
 // The list cut into groups that share their launches and, one after the other,
@@ -1048,7 +1050,9 @@ struct Runner {
             a += n * steps * (3 * s * s * L + s * s * s);
             b += n * (5 * s * s * L + 3 * std::max(1, 4 * steps - 3) * s * s * s);
         }
-        return a < b;
+        // (MFMAs of both; single steps are a few launches more: bf16 512 x 1024 151 us and 162
+        // in blocks, 1024 x 1024 199 and 255, but 1024 x 4096 320 and 286)
+        return a < 0.75 * b;
     }
     hipError_t go_direct(int steps, const double* coef) {
         double lambda = 1.0;
