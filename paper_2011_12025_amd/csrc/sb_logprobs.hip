@@ -15,6 +15,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "sb_common.h"
 #include "sb_kernels.h"
@@ -59,16 +60,29 @@ __device__ __forceinline__ void add(Acc& a, float z) {
     a.t += e * fmaxf(d, FAR);
 }
 
+// The maximum or the sum of the lanes' values, in a fixed order, by DPP: prefixes of
+// rows of 16 lanes, then of the rows; `none` where a lane has no neighbour.
+template <bool MAX>
+__device__ __forceinline__ float wave_total(float v, float none) {
+    auto step = [&](auto ctrl, auto rows) {
+        const float o = __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(none), __float_as_int(v),
+                                                                   decltype(ctrl)::value, decltype(rows)::value, 0xF, false));
+        v = MAX ? fmaxf(v, o) : v + o;
+    };
+    constexpr std::integral_constant<int, 0xF> all{};
+    step(std::integral_constant<int, 0x111>{}, all);  // row_shr 1, 2, 4, 8
+    step(std::integral_constant<int, 0x112>{}, all);
+    step(std::integral_constant<int, 0x114>{}, all);
+    step(std::integral_constant<int, 0x118>{}, all);
+    step(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xA>{});  // row_bcast 15, 31
+    step(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xC>{});
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+
 __device__ __forceinline__ Acc wave_join(Acc a) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-        Acc b;
-        b.m = __shfl_xor(a.m, o, 64);
-        b.s = __shfl_xor(a.s, o, 64);
-        b.t = __shfl_xor(a.t, o, 64);
-        join(a, b);
-    }
-    return a;
+    const float m = wave_total<true>(a.m, LOWEST);
+    raise(a, m);
+    return Acc{m, wave_total<false>(a.s, 0.0f), wave_total<false>(a.t, 0.0f)};
 }
 
 // Order of the alternatives as one integer: the larger score, then the lower
@@ -143,8 +157,18 @@ struct Part {  // results of a part of a row in the workspace, followed by topk 
 };
 __host__ __device__ inline long long part_bytes(int topk) { return 16 + 8LL * topk; }
 
-// The k-th largest of the lanes' values.
+// The k-th largest of the lanes' values: the largest k times over where that is
+// less than ranking all (about 14 instructions a time, 320 to rank).
 __device__ __forceinline__ float kth_of_lanes(float m, int k) {
+    if (k <= 16) {
+        float left = m, top = -INFINITY;
+        for (int i = 0; i < k; ++i) {
+            top = wave_total<true>(left, -INFINITY);
+            const int at = __ffsll((unsigned long long)__ballot(left == top)) - 1;
+            left = lane_id() == at ? -INFINITY : left;
+        }
+        return top;
+    }
     int rank = 0;
 #pragma unroll 16
     for (int l = 0; l < 64; ++l) {
@@ -773,9 +797,11 @@ __global__ __launch_bounds__(256) void k_logp_grad_planes(LogpGradArgs a, int pe
 // Host side
 // ---------------------------------------------------------------------------
 // Rows for one thread each: short ones, staged as they lie (with the channels
-// of the buffer that are no classes).  Returns rows of a workgroup, or 0.
+// of the buffer that are no classes), past 64 classes where they are many (bf16, a
+// thread and a wave a row: 60000 x 100 11 us and over 50, 8192 x 100 14.6 and 13.4).
+// Returns rows of a workgroup, or 0.
 int short_rows(int es, long long R, int C, long long ld, bool grad) {
-    if (ld > 2LL * C || C > 1024 || (C > 64 && R < 16384)) return 0;
+    if (ld > 2LL * C || C > 128 || (C > 64 && R < 16384)) return 0;
     for (int rows = 256; rows >= 64; rows /= 2)
         if (staged_bytes((int)std::min<long long>(rows * ld * es, 1 << 20)) + (grad ? staged_bytes(rows * C * es) : 0) <=
             (rows == 64 ? 48 : 24) * 1024)
@@ -783,9 +809,18 @@ int short_rows(int es, long long R, int C, long long ld, bool grad) {
     return 0;
 }
 
-int row_waves(long long R, int C) { return C <= 1024 ? 1 : C <= 16384 || R >= 512 ? 4 : 16; }
+// Waves of a row.  One, four of them a workgroup, where the rows fill the chip
+// and are at most 16 KB (4096 rows, one and four waves: 2048 bf16 classes 6.0 and
+// 12.1 us, 8192 18.3 and 19.2, fp32 8192 23.1 and 21.8), sixteen for few long ones
+// (256 x 50001 bf16: 10.9, with four 19.6).
+int row_waves(int es, long long R, int C) {
+    if (C <= 1024 || (C * (long long)es <= 16384 && R >= 1024)) return 1;
+    return C <= 16384 || R >= 512 ? 4 : 16;
+}
 
-// Parts of a long row where the rows alone leave most of the chip idle.
+// Parts of a long row where the rows alone leave most of the chip idle (131072 bf16
+// classes, split and not: one row 11.2 and 19.7 us, 32 rows 17.7 and 21.7; 65536
+// 13.0 and 14.3, 32000 12.6 and 11.3).
 int row_parts(long long R, int C) {
     if (C < 65536 || R >= 64) return 1;
     return (int)std::min<long long>({MAX_PARTS, C / 16384, 256 / R});
@@ -857,7 +892,7 @@ hipError_t logp_t(const LogpArgs& a, Ws ws, hipStream_t st) {
         hipLaunchKernelGGL(k_logp_join<T>, dim3((unsigned)a.R), dim3(256), 0, st, a, parts, (const char*)ws.p);
         return hipGetLastError();
     }
-    const int nw = row_waves(a.R, a.C);
+    const int nw = row_waves(sizeof(T), a.R, a.C);
     if (nw == 1) return logp_rows<T, 1>(a, ws, st, 1);
     return nw == 4 ? logp_rows<T, 4>(a, ws, st, 1) : logp_rows<T, 16>(a, ws, st, 1);
 }
