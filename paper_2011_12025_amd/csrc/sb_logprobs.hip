@@ -147,6 +147,10 @@ struct TopList {
 // 1024 for 20 alternatives of random scores); their vectors are read again, and
 // the scores that reach the bound sorted into a list.  The pass over the row costs
 // what it does without alternatives.
+//
+// PLANES: a wave takes a pixel of a plane, its classes a plane apart and one score a
+// "vector".  For more alternatives than the registers of a thread hold: 36 pixels
+// of 532 classes with 20 alternatives, listed in LDS by a thread a pixel, took 300 us.
 // ---------------------------------------------------------------------------
 constexpr int LU = 4;
 
@@ -179,8 +183,8 @@ __device__ __forceinline__ float kth_of_lanes(float m, int k) {
     return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(m), at));
 }
 
-template <typename T, bool ENT>
-__device__ __forceinline__ void add_vectors(Acc& a, const float (&f)[LU][LV<T>], const float (&vm)[LU]) {
+template <bool ENT, int V>
+__device__ __forceinline__ void add_vectors(Acc& a, const float (&f)[LU][V], const float (&vm)[LU]) {
     float m2 = a.m;
 #pragma unroll
     for (int u = 0; u < LU; ++u) m2 = fmaxf(m2, vm[u]);
@@ -189,18 +193,19 @@ __device__ __forceinline__ void add_vectors(Acc& a, const float (&f)[LU][LV<T>],
 #pragma unroll
     for (int u = 0; u < LU; ++u)
 #pragma unroll
-        for (int i = 0; i < LV<T>; ++i) {
+        for (int i = 0; i < V; ++i) {
             const float d = (f[u][i] - m2) * LOG2E, e = exp2_(d);  // (NaN stays in e)
-            s[i & 1] += e;
-            if (ENT) t[i & 1] = fmaf(e, fmaxf(d, FAR), t[i & 1]);
+            s[(u + i) & 1] += e;
+            if (ENT) t[(u + i) & 1] = fmaf(e, fmaxf(d, FAR), t[(u + i) & 1]);
         }
     a.s += s[0] + s[1];
     if (ENT) a.t += t[0] + t[1];
 }
 
-template <typename T, int NW, bool TOP, bool ENT>
+template <typename T, int NW, bool TOP, bool ENT, bool PLANES = false>
 __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void k_logp_rows(LogpArgs a, int parts, char* ws) {
-    constexpr int V = LV<T>, THREADS = NW == 1 ? 256 : NW * 64;
+    static_assert(!PLANES || NW == 1, "a wave a pixel");
+    constexpr int V = PLANES ? 1 : LV<T>, THREADS = NW == 1 ? 256 : NW * 64;
     __shared__ float s_acc[3][NW];
     __shared__ u64 s_key[TOP && NW > 1 ? NW * 64 : 1];
     __shared__ float s_max[TOP && NW > 1 ? NW * 64 : 1];
@@ -212,10 +217,11 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void k_logp_rows(LogpArgs 
     const long long r = NW == 1 ? item : item / parts;
     const int part = NW == 1 ? 0 : (int)(item - r * parts);
     if (r >= a.R) return;  // (NW = 1 alone: whole waves, and no barrier follows)
-    const T* z = (const T*)a.z + r * a.C_buf;
+    const long long n = PLANES ? r / a.P : r, p = PLANES ? r - n * a.P : 0, P = PLANES ? a.P : 1;
+    const T* z = (const T*)a.z + n * a.C_buf * P + p;
 
     // [0, head) and [tail, C) score by score, whole vectors between
-    const int head = min(a.C, (int)((16 - (reinterpret_cast<uintptr_t>(z) & 15)) & 15) / (int)sizeof(T));
+    const int head = PLANES ? 0 : min(a.C, (int)((16 - (reinterpret_cast<uintptr_t>(z) & 15)) & 15) / (int)sizeof(T));
     const int nv = (a.C - head) / V, tail = head + nv * V;
     const int v0 = (int)((long long)nv * part / parts), v1 = (int)((long long)nv * (part + 1) / parts);
     const T* zv = z + head;
@@ -225,13 +231,17 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void k_logp_rows(LogpArgs 
     const bool in_h = lane < head, in_t = tail + lane < a.C;
     const float fh = first && in_h ? to_f32(z[lane]) : -INFINITY, ft = final_ && in_t ? to_f32(z[tail + lane]) : -INFINITY;
 
-    typename RawT<16>::type cur[LU], nxt[LU];
+    Vec<T, V> cur[LU], nxt[LU];
     constexpr int STEP = NW * 64 * LU;
-    auto load = [&](typename RawT<16>::type(&to)[LU], int base) {
+    auto load = [&](Vec<T, V>(&to)[LU], int base) {
 #pragma unroll
         for (int u = 0; u < LU; ++u) {
             const int v = base + u * 64 + lane;
-            if (v < v1) to[u] = ld_nt16(zv + (long long)v * V);
+            if constexpr (PLANES) {
+                if (v < v1) to[u].e[0] = zv[v * P];
+            } else {
+                if (v < v1) to[u].raw = ld_nt16(zv + (long long)v * V);
+            }
         }
     };
     const int begin = v0 + wave * (64 * LU);
@@ -241,16 +251,14 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void k_logp_rows(LogpArgs 
         float f[LU][V], vm[LU];
 #pragma unroll
         for (int u = 0; u < LU; ++u) {
-            Vec<T, V> q;
-            q.raw = cur[u];
             const bool in = base + u * 64 + lane < v1;
 #pragma unroll
-            for (int i = 0; i < V; ++i) f[u][i] = in ? to_f32(q.e[i]) : -INFINITY;
+            for (int i = 0; i < V; ++i) f[u][i] = in ? to_f32(cur[u].e[i]) : -INFINITY;
             vm[u] = f[u][0];
 #pragma unroll
             for (int i = 1; i < V; ++i) vm[u] = fmaxf(vm[u], f[u][i]);
         }
-        add_vectors<T, ENT>(acc, f, vm);
+        add_vectors<ENT, V>(acc, f, vm);
 #pragma unroll
         for (int u = 0; u < LU; ++u) cur[u] = nxt[u];
     }
@@ -297,9 +305,8 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void k_logp_rows(LogpArgs 
                 const int of = __shfl(which, min(ci, 63), 64);
                 const int v = begin + t / LU * STEP + t % LU * 64 + of;
                 const bool in = ci < min(count, c0 + together) && t < nt && v < v1;
-                Vec<T, V> q;
-                q.raw = uint4{0u, 0u, 0u, 0u};
-                if (in) q.raw = *reinterpret_cast<const uint4*>(zv + (long long)v * V);
+                Vec<T, V> q = vzero<T, V>();
+                if (in) q = PLANES ? vload<T, V>(zv + v * P) : vload<T, V>(zv + (long long)v * V);
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
                     const float f = to_f32(q.e[i]);
@@ -334,8 +341,9 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void k_logp_rows(LogpArgs 
         if (out) {
             ((u64*)(out + 1))[i] = k;
         } else {
-            a.top_logp[r * a.topk + i] = row.logp(key_score(k));
-            a.top_index[r * a.topk + i] = key_class(k);
+            const long long at = (n * a.topk + i) * P + p;
+            a.top_logp[at] = row.logp(key_score(k));
+            a.top_index[at] = key_class(k);
         }
     };
     if (TOP) {
@@ -363,7 +371,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void k_logp_rows(LogpArgs 
     if (ENT) a.entropy[r] = row.entropy(acc);
     if (a.labels) {
         const long long t = a.labels[r];
-        a.logp[r] = t == a.ignore ? 0.0f : t < 0 || t >= a.C ? NAN : row.logp(to_f32(z[t]));
+        a.logp[r] = t == a.ignore ? 0.0f : t < 0 || t >= a.C ? NAN : row.logp(to_f32(z[t * P]));
     }
 }
 
@@ -405,8 +413,8 @@ __global__ __launch_bounds__(256) void k_logp_join(LogpArgs a, int parts, const 
 
 // ---------------------------------------------------------------------------
 // One thread a row (or a few waves, each with a range of its classes): scores
-// come eight at a time, the alternatives are a sorted list in registers
-// (K <= 8) or in LDS.  Used where rows are short or where neighbouring rows are
+// come eight at a time, the alternatives (K <= 16) are a sorted list in registers.
+// Used where rows are short or where neighbouring rows are
 // neighbours in memory (the pixels of a plane).
 // ---------------------------------------------------------------------------
 // Order of two scores as integers; INT_MIN is below all.
@@ -421,7 +429,7 @@ __device__ __forceinline__ float rank_score(int k) {
 template <int K>
 struct RegTop {  // classes come in rising order: an equal score stays behind
     int k[K], j[K];
-    __device__ __forceinline__ RegTop(int*, int) {
+    __device__ __forceinline__ RegTop() {
 #pragma unroll
         for (int i = 0; i < K; ++i) {
             k[i] = INT_MIN;
@@ -457,35 +465,10 @@ struct RegTop {  // classes come in rising order: an equal score stays behind
 };
 template <>
 struct RegTop<0> {
-    __device__ __forceinline__ RegTop(int*, int) {}
     __device__ __forceinline__ void put(int, int) {}
     __device__ __forceinline__ int key(int) const { return 0; }
     __device__ __forceinline__ int cls(int) const { return 0; }
 };
-// topk (key, class) pairs of this thread in LDS, 64 words between those of a lane.
-template <>
-struct RegTop<-1> {
-    int* p;
-    int n, last;
-    __device__ __forceinline__ RegTop(int* lds, int topk) : p(lds + lane_id()), n(topk), last(INT_MIN) {
-        for (int i = 0; i < n; ++i) p[128 * i] = INT_MIN;
-    }
-    __device__ __forceinline__ void put(int key, int cls) {
-        if (key <= last) return;
-        int i = n - 1;
-        for (; i > 0 && key > p[128 * (i - 1)]; --i) {
-            p[128 * i] = p[128 * (i - 1)];
-            p[128 * i + 64] = p[128 * (i - 1) + 64];
-        }
-        p[128 * i] = key;
-        p[128 * i + 64] = cls;
-        last = p[128 * (n - 1)];
-    }
-    __device__ __forceinline__ int key(int i) const { return p[128 * i]; }
-    __device__ __forceinline__ int cls(int i) const { return p[128 * i + 64]; }
-};
-__host__ __device__ constexpr int top_lds(int topk) { return 512 * topk; }  // bytes of a wave's lists
-
 template <int K, bool ENT, bool FULL, typename Get>
 __device__ __forceinline__ void scan8(Get get, int c, int c1, Acc& a, RegTop<K>& top) {
     float f[8];
@@ -552,18 +535,18 @@ __device__ __forceinline__ void stage_in(const T* src, int n, char* lds) {
 // Short rows (NHWC, tokens): a workgroup stages blockDim rows as they lie and
 // each thread goes through one.
 template <typename T, int K, bool ENT>
-__global__ __launch_bounds__(256) void k_logp_short(LogpArgs a, int lists) {
+__global__ __launch_bounds__(256) void k_logp_short(LogpArgs a) {
     extern __shared__ __align__(16) char lds[];
     const int tid = (int)threadIdx.x, rows = (int)blockDim.x;
     const long long r0 = (long long)blockIdx.x * rows;
     const int nr = (int)min((long long)rows, a.R - r0), ld = (int)a.C_buf;
-    stage_in((const T*)a.z + r0 * ld, (nr - 1) * ld + a.C, lds + lists);
+    stage_in((const T*)a.z + r0 * ld, (nr - 1) * ld + a.C, lds);
     __syncthreads();
     if (tid >= nr) return;
     const int at = tid * ld * (int)sizeof(T);
-    auto get = [&](int c) { return to_f32(*(const T*)(lds + lists + staged(at + c * (int)sizeof(T)))); };
+    auto get = [&](int c) { return to_f32(*(const T*)(lds + staged(at + c * (int)sizeof(T)))); };
     Acc acc = nothing();
-    RegTop<K> top((int*)(lds + (tid >> 6) * top_lds(a.topk)), a.topk);
+    RegTop<K> top;
     scan<K, ENT>(get, 0, a.C, acc, top);
     row_out<K, ENT>(a, r0 + tid, r0 + tid, 0, acc, top, get);
 }
@@ -571,8 +554,8 @@ __global__ __launch_bounds__(256) void k_logp_short(LogpArgs a, int lists) {
 // Pixels of planes (NCHW): 64 neighbouring pixels a wave; NW waves share them
 // and split the classes, so that small maps fill the chip too.
 template <typename T, int K, bool ENT, int NW>
-__global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void k_logp_planes(LogpArgs a, int lists) {
-    extern __shared__ __align__(16) char lds[];  // lists, then the waves' results
+__global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void k_logp_planes(LogpArgs a) {
+    extern __shared__ __align__(16) char lds[];  // the waves' results
     const int lane = lane_id(), wid = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int wave = NW == 1 ? 0 : wid;
     const long long r = ((long long)blockIdx.x * (NW == 1 ? 4 : 1) + (NW == 1 ? wid : 0)) * 64 + lane;
@@ -581,11 +564,11 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void k_logp_planes(LogpArg
     const T* z = (const T*)a.z + n * a.C_buf * a.P + p;
     auto get = [&](int c) { return to_f32(z[c * a.P]); };
     Acc acc = nothing();
-    RegTop<K> top((int*)(lds + wid * top_lds(a.topk)), a.topk);
+    RegTop<K> top;
     scan<K, ENT>(get, (int)((long long)a.C * wave / NW), (int)((long long)a.C * (wave + 1) / NW), acc, top);
     if constexpr (NW > 1) {
-        float* res = (float*)(lds + lists);  // [wave][3][64]
-        int* keys = (int*)(res + NW * 192);  // [wave][topk][2][64] of register lists
+        float* res = (float*)lds;            // [wave][3][64]
+        int* keys = (int*)(res + NW * 192);  // [wave][topk][2][64]
         res[wave * 192 + lane] = acc.m;
         res[wave * 192 + 64 + lane] = acc.s;
         res[wave * 192 + 128 + lane] = acc.t;
@@ -602,8 +585,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void k_logp_planes(LogpArg
             join(acc, Acc{res[w * 192 + lane], res[w * 192 + 64 + lane], res[w * 192 + 128 + lane]});
             if (K != 0)
                 for (int i = 0; i < a.topk; ++i) {
-                    const int* q = K > 0 ? keys + ((w * a.topk + i) * 2) * 64 + lane
-                                         : (const int*)(lds + w * top_lds(a.topk)) + 128 * i + lane;
+                    const int* q = keys + ((w * a.topk + i) * 2) * 64 + lane;
                     if (q[0] != INT_MIN) top.put(q[0], q[64]);
                 }
         }
@@ -633,6 +615,7 @@ struct GradRow {
         gh = a.d_entropy ? a.d_entropy[r] : 0.0f;
         H = a.d_entropy ? a.entropy[r] : 0.0f;
         G = g;
+#pragma unroll 8
         for (int i = 0; i < a.topk; ++i) {
             const long long q = (n * a.topk + i) * a.P + p;
             const int j = a.top_index[q];
@@ -657,9 +640,11 @@ struct GradRow {
         float d = all(z);
         if (empty) return d;
         if (j == label) d += g;
+#pragma unroll 8
         for (int i = 0; i < a.topk; ++i) {
             const long long q = (n * a.topk + i) * a.P + p;
-            if (a.top_index[q] == j) d += a.d_top[q];
+            const float gi = a.d_top[q];  // (read either way: the loads of several go out together)
+            d += a.top_index[q] == j ? gi : 0.0f;
         }
         return d;
     }
@@ -738,7 +723,7 @@ __global__ __launch_bounds__(256) void k_logp_grad_short(LogpGradArgs a, int out
         GradRow row(a, r, r, 0);
         if (row.far()) {
             Acc acc = nothing();
-            RegTop<0> none(nullptr, 0);
+            RegTop<0> none;
             scan<0, false>(get, 0, a.C, acc, none);
             row.take(acc);
         }
@@ -780,7 +765,7 @@ __global__ __launch_bounds__(256) void k_logp_grad_planes(LogpGradArgs a, int pe
     GradRow row(a, r, n, p);
     if (row.far()) {
         Acc acc = nothing();
-        RegTop<0> none(nullptr, 0);
+        RegTop<0> none;
         scan<0, false>(get, 0, a.C, acc, none);
         row.take(acc);
     }
@@ -802,7 +787,8 @@ __global__ __launch_bounds__(256) void k_logp_grad_planes(LogpGradArgs a, int pe
 // Returns rows of a workgroup, or 0.
 int short_rows(int es, long long R, int C, long long ld, bool grad) {
     if (ld > 2LL * C || C > 128 || (C > 64 && R < 16384)) return 0;
-    for (int rows = 256; rows >= 64; rows /= 2)
+    // (a workgroup takes fewer where all would leave CUs idle)
+    for (int rows = R >= 65536 ? 256 : R >= 32768 ? 128 : 64; rows >= 64; rows /= 2)
         if (staged_bytes((int)std::min<long long>(rows * ld * es, 1 << 20)) + (grad ? staged_bytes(rows * C * es) : 0) <=
             (rows == 64 ? 48 : 24) * 1024)
             return rows;
@@ -826,6 +812,10 @@ int row_parts(long long R, int C) {
     return (int)std::min<long long>({MAX_PARTS, C / 16384, 256 / R});
 }
 
+// Whether a thread keeps the alternatives in registers (else a wave a row sorts
+// them): 16 of them cost 80 instructions a class, which a short row has few of.
+bool reg_top(int topk, int C) { return topk <= 8 || (topk <= 16 && C <= 64); }
+
 bool is_planes(long long P) { return P > 1; }
 
 template <typename T, int K>
@@ -833,13 +823,10 @@ hipError_t logp_k(const LogpArgs& a, hipStream_t st, int rows, bool planes) {
     const bool ent = a.entropy != nullptr;
     const int es = sizeof(T);
     if (!planes) {
-        const int lists = K < 0 ? rows / 64 * top_lds(a.topk) : 0;
-        const int lds = lists + staged_bytes(((rows - 1) * (int)a.C_buf + a.C) * es + 16);
+        const int lds = staged_bytes(((rows - 1) * (int)a.C_buf + a.C) * es + 16);
         const unsigned grid = (unsigned)((a.R + rows - 1) / rows);
         auto run = [&](auto kernel) -> hipError_t {
-            if (lds > 64 * 1024)
-                if (hipError_t e = ensure_dyn_lds((const void*)kernel, lds); e != hipSuccess) return e;
-            hipLaunchKernelGGL(kernel, dim3(grid), dim3(rows), lds, st, a, lists);
+            hipLaunchKernelGGL(kernel, dim3(grid), dim3(rows), lds, st, a);
             return hipGetLastError();
         };
         return ent ? run(k_logp_short<T, K, true>) : run(k_logp_short<T, K, false>);
@@ -849,18 +836,15 @@ hipError_t logp_k(const LogpArgs& a, hipStream_t st, int rows, bool planes) {
     const int nw = waves >= 4096 || a.C < 32 ? 1 : waves >= 1024 || a.C < 128 ? 4 : 16;
     auto run = [&](auto kernel, int w) -> hipError_t {
         const int all = w == 1 ? 4 : w;
-        const int lists = K < 0 ? all * top_lds(a.topk) : 0;
-        const int lds = lists + (w > 1 ? w * 768 + (K > 0 ? w * a.topk * 512 : 0) : 0);
+        const int lds = w > 1 ? w * 768 + w * a.topk * 512 : 0;
         const unsigned grid = (unsigned)(w == 1 ? (waves + 3) / 4 : waves);
         if (lds > 64 * 1024)
             if (hipError_t e = ensure_dyn_lds((const void*)kernel, lds); e != hipSuccess) return e;
-        hipLaunchKernelGGL(kernel, dim3(grid), dim3(all * 64), lds, st, a, lists);
+        hipLaunchKernelGGL(kernel, dim3(grid), dim3(all * 64), lds, st, a);
         return hipGetLastError();
     };
-    // (lists of 64 alternatives take 32 KB a wave: four waves at most)
-    if (nw == 16 && !(K < 0 && a.topk > 16))
-        return ent ? run(k_logp_planes<T, K, true, 16>, 16) : run(k_logp_planes<T, K, false, 16>, 16);
-    if (nw >= 4) return ent ? run(k_logp_planes<T, K, true, 4>, 4) : run(k_logp_planes<T, K, false, 4>, 4);
+    if (nw == 16) return ent ? run(k_logp_planes<T, K, true, 16>, 16) : run(k_logp_planes<T, K, false, 16>, 16);
+    if (nw == 4) return ent ? run(k_logp_planes<T, K, true, 4>, 4) : run(k_logp_planes<T, K, false, 4>, 4);
     return ent ? run(k_logp_planes<T, K, true, 1>, 1) : run(k_logp_planes<T, K, false, 1>, 1);
 }
 
@@ -877,13 +861,18 @@ hipError_t logp_rows(const LogpArgs& a, Ws ws, hipStream_t st, int parts) {
 template <typename T>
 hipError_t logp_t(const LogpArgs& a, Ws ws, hipStream_t st) {
     const bool planes = is_planes(a.P);
+    if (planes && !reg_top(a.topk, a.C)) {
+        const dim3 grid((unsigned)((a.R + 3) / 4));
+        auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, a, 1, (char*)nullptr); };
+        a.entropy ? run(k_logp_rows<T, 1, true, true, true>) : run(k_logp_rows<T, 1, true, false, true>);
+        return hipGetLastError();
+    }
     const int rows = planes ? 0 : short_rows(sizeof(T), a.R, a.C, a.C_buf, false);
-    if (planes || (rows && (a.topk <= 8 || rows / 64 * top_lds(a.topk) <= 64 * 1024))) {
+    if (planes || (rows && reg_top(a.topk, a.C))) {
         if (a.topk == 0) return logp_k<T, 0>(a, st, rows, planes);
         if (a.topk == 1) return logp_k<T, 1>(a, st, rows, planes);
         if (a.topk <= 4) return logp_k<T, 4>(a, st, rows, planes);
-        if (a.topk <= 8) return logp_k<T, 8>(a, st, rows, planes);
-        return logp_k<T, -1>(a, st, rows, planes);
+        return a.topk <= 8 ? logp_k<T, 8>(a, st, rows, planes) : logp_k<T, 16>(a, st, rows, planes);
     }
     const int parts = row_parts(a.R, a.C);
     if (parts > 1) {

@@ -129,6 +129,7 @@ def test_rows(R, C, of, skip, topk, dtype):
 MAPS = [  # N, C, H, W, buffer, topk
     (1, 19, 16, 32, 24, 1), (2, 5, 7, 9, 5, 3), (1, 150, 33, 47, 152, 10), (2, 1, 4, 4, 1, 1), (3, 300, 5, 3, 304, 20),
     (1, 1000, 7, 7, 1000, 5), (1, 40, 300, 301, 40, 0), (2, 8, 1, 1, 8, 2), (1, 70, 1, 40, 70, 64), (1, 129, 64, 65, 130, 8),
+    (2, 13, 25, 44, 13, 13), (1, 60, 9, 11, 64, 16), (1, 532, 9, 4, 532, 20),
 ]
 
 
