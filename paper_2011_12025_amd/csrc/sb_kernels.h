@@ -201,6 +201,7 @@ struct LogpArgs {
     int* top_index;
     long long R, P, C_buf, ignore;
     int C, topk;
+    long long r0;  // (of a launch: its first row)
 };
 struct LogpGradArgs {
     const void* z;
@@ -210,6 +211,7 @@ struct LogpGradArgs {
     const int* top_index;
     long long R, P, C_buf, C_dbuf, ignore;
     int C, topk;
+    long long r0;  // (of a launch: its first row)
 };
 int logp_max_top();
 size_t logp_ws_bytes(int dtype, const LogpArgs& a);

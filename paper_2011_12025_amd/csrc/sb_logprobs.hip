@@ -213,7 +213,7 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void k_logp_rows(LogpArgs 
     __shared__ int s_n, s_nan;
     const int lane = lane_id(), wid = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int wave = NW == 1 ? 0 : wid;
-    const long long item = NW == 1 ? (long long)blockIdx.x * 4 + wid : (long long)blockIdx.x;
+    const long long item = NW == 1 ? a.r0 + (long long)blockIdx.x * 4 + wid : a.r0 * parts + blockIdx.x;
     const long long r = NW == 1 ? item : item / parts;
     const int part = NW == 1 ? 0 : (int)(item - r * parts);
     if (r >= a.R) return;  // (NW = 1 alone: whole waves, and no barrier follows)
@@ -654,8 +654,9 @@ struct GradRow {
 template <typename T>
 __global__ __launch_bounds__(256) void k_logp_grad_rows(LogpGradArgs a, int chunks, int per) {
     constexpr int V = LV<T>;
-    const long long r = blockIdx.x / (unsigned)chunks;
-    const int chunk = (int)(blockIdx.x - (unsigned)r * chunks), tid = (int)threadIdx.x;
+    const unsigned row_in = blockIdx.x / (unsigned)chunks;
+    const long long r = a.r0 + row_in;
+    const int chunk = (int)(blockIdx.x - row_in * chunks), tid = (int)threadIdx.x;
     const T* z = (const T*)a.z + r * a.C_buf;
     T* dz = (T*)a.dz + r * a.C_dbuf;
     GradRow row(a, r, r, 0);
@@ -848,25 +849,29 @@ hipError_t logp_k(const LogpArgs& a, hipStream_t st, int rows, bool planes) {
     return ent ? run(k_logp_planes<T, K, true, 1>, 1) : run(k_logp_planes<T, K, false, 1>, 1);
 }
 
-template <typename T, int NW>
-hipError_t logp_rows(const LogpArgs& a, Ws ws, hipStream_t st, int parts) {
-    const long long items = NW == 1 ? (a.R + 3) / 4 : a.R * parts;
-    const dim3 grid((unsigned)items), block(NW == 1 ? 256 : NW * 64);
-    auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, a, parts, (char*)ws.p); };
-    if (a.topk) a.entropy ? run(k_logp_rows<T, NW, true, true>) : run(k_logp_rows<T, NW, true, false>);
-    else a.entropy ? run(k_logp_rows<T, NW, false, true>) : run(k_logp_rows<T, NW, false, false>);
-    return hipGetLastError();
+// A launch holds less than 2^32 threads: rows with a wave or more each go in pieces.
+constexpr long long MAX_THREADS = 1LL << 31;
+
+template <typename T, int NW, bool PLANES = false>
+hipError_t logp_rows(LogpArgs a, Ws ws, hipStream_t st, int parts) {
+    const long long piece = MAX_THREADS / (NW * 64) / parts;
+    for (; a.r0 < a.R; a.r0 += piece) {
+        const long long rows = std::min(piece, a.R - a.r0), items = NW == 1 ? (rows + 3) / 4 : rows * parts;
+        const dim3 grid((unsigned)items), block(NW == 1 ? 256 : NW * 64);
+        auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, a, parts, (char*)ws.p); };
+        if constexpr (PLANES)
+            a.entropy ? run(k_logp_rows<T, NW, true, true, true>) : run(k_logp_rows<T, NW, true, false, true>);
+        else if (a.topk) a.entropy ? run(k_logp_rows<T, NW, true, true>) : run(k_logp_rows<T, NW, true, false>);
+        else a.entropy ? run(k_logp_rows<T, NW, false, true>) : run(k_logp_rows<T, NW, false, false>);
+        if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 template <typename T>
 hipError_t logp_t(const LogpArgs& a, Ws ws, hipStream_t st) {
     const bool planes = is_planes(a.P);
-    if (planes && !reg_top(a.topk, a.C)) {
-        const dim3 grid((unsigned)((a.R + 3) / 4));
-        auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, a, 1, (char*)nullptr); };
-        a.entropy ? run(k_logp_rows<T, 1, true, true, true>) : run(k_logp_rows<T, 1, true, false, true>);
-        return hipGetLastError();
-    }
+    if (planes && !reg_top(a.topk, a.C)) return logp_rows<T, 1, true>(a, ws, st, 1);
     const int rows = planes ? 0 : short_rows(sizeof(T), a.R, a.C, a.C_buf, false);
     if (planes || (rows && reg_top(a.topk, a.C))) {
         if (a.topk == 0) return logp_k<T, 0>(a, st, rows, planes);
@@ -905,11 +910,16 @@ hipError_t grad_t(const LogpGradArgs& a, hipStream_t st) {
         return hipGetLastError();
     }
     // ranges of 4 vectors a thread, or 16 where rows are many
-    int per = 256 * LV<T> * (a.R * a.C >= (64LL << 20) ? 16 : 4);
-    while (a.R * ((a.C + per - 1) / per) >= (1LL << 31)) per *= 2;
-    const int chunks = (a.C + per - 1) / per;
-    hipLaunchKernelGGL(k_logp_grad_rows<T>, dim3((unsigned)(a.R * chunks)), dim3(256), 0, st, a, chunks, per);
-    return hipGetLastError();
+    const int per = 256 * LV<T> * (a.R * a.C >= (64LL << 20) ? 16 : 4);
+    const int chunks = (int)(((long long)a.C + per - 1) / per);
+    const long long piece = std::max(1LL, MAX_THREADS / 256 / chunks);
+    LogpGradArgs b = a;
+    for (; b.r0 < b.R; b.r0 += piece) {
+        const long long rows = std::min(piece, b.R - b.r0);
+        hipLaunchKernelGGL(k_logp_grad_rows<T>, dim3((unsigned)(rows * chunks)), dim3(256), 0, st, b, chunks, per);
+        if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace

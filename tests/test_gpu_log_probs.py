@@ -354,6 +354,28 @@ def test_batches_of_sequences_strides_and_nothing():
     assert torch.equal(a, b)
 
 
+def test_rows_past_32_bits():
+    """More rows than threads of one launch, and offsets past 2^32 elements: the last rows, forward and backward."""
+    R, C = (1 << 25) + 70, 132
+    if torch.cuda.mem_get_info()[0] < 60 << 30:
+        pytest.skip("needs 60 GB of free memory")
+    log(f"[log_probs] {R} rows of {C}")
+    z = torch.empty(R, C, dtype=torch.float16, device="cuda").normal_(0, 2.5)
+    lab = torch.zeros(R, dtype=torch.int64, device="cuda")
+    lab[-200:] = torch.arange(200, device="cuda") % C
+    logp, lse, H, tl, ti = sb.log_probs(z, lab, topk=2)
+    dz = sb.log_probs_backward(z, lab, lse, d_logp=torch.ones_like(logp))
+    torch.cuda.synchronize()
+    for at in (slice(0, 200), slice(R // 2, R // 2 + 200), slice(R - 200, R)):
+        r64, l64 = z[at].double().cpu(), lab[at].cpu()
+        e_logp, e_lse, e_H, e_tl, e_ti = reference(r64, l64, 2, -100)
+        close(logp[at], e_logp, 1e-4, "logp")
+        close(H[at], e_H, 1e-4, "entropy")
+        assert torch.equal(ti[at].cpu().long(), e_ti)
+        ref, size = grad_reference(r64, l64, torch.ones(200, dtype=torch.float64), None, None, None, -100)
+        close(dz[at], ref, 2.0 ** -11 * ref.abs() * (1 + 2.0 ** -8) + 2.0 ** -25 + 2.0 ** -16 * size, "dlogits")
+
+
 @pytest.mark.parametrize("bad", ["labels type", "labels shape", "topk", "topk classes", "columns", "rows", "overlap",
                                  "no gradient", "entropy", "workspace", "dtype", "cpu"])
 def test_refusals(bad):
