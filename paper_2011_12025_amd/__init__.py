@@ -848,9 +848,11 @@ def _buf_channels(t: torch.Tensor, layout: int) -> int:
     return c
 
 
-def _matrix(t: torch.Tensor):
+def _matrix(t: torch.Tensor, like=None):
     """(batch, rows, cols, distance of rows, distance of matrices) of an update
-    in row-major memory; a matrix in column-major memory is taken transposed."""
+    in row-major memory; a matrix in column-major memory is taken transposed.
+    like: (batch, rows, cols) to be read as, where the memory can be read in both
+    ways (a single row or column)."""
     if t.dim() == 4:
         layout_of(t)  # contiguous or channels_last: filters of C_out rows either way
         n = t.shape[1] * t.shape[2] * t.shape[3]
@@ -862,11 +864,19 @@ def _matrix(t: torch.Tensor):
     batch, sb = (t.shape[0], t.stride(0)) if t.dim() == 3 else (1, 0)
     if batch == 1:
         sb = 0
+    ways = []
     if (n == 1 or sn == 1) and (m == 1 or sm >= n):
-        return batch, m, n, sm if m > 1 else n, sb
+        ways.append((batch, m, n, sm if m > 1 else n, sb))
     if (m == 1 or sm == 1) and (n == 1 or sn >= m):
-        return batch, n, m, sn if n > 1 else m, sb
-    raise ValueError("the rows or the columns of an update must be contiguous")
+        ways.append((batch, n, m, sn if n > 1 else m, sb))
+    if not ways:
+        raise ValueError("the rows or the columns of an update must be contiguous")
+    if like is None:
+        return ways[0]
+    for w in ways:
+        if w[:3] == like:
+            return w
+    raise ValueError("out must have its update's order of rows and columns")
 
 
 def _matrices(updates, outs=None):
@@ -878,9 +888,7 @@ def _matrices(updates, outs=None):
         if outs is None:
             q.ld_out, q.batch_stride_out = q.cols, q.rows * q.cols
         else:
-            batch, rows, cols, q.ld_out, q.batch_stride_out = _matrix(outs[i])
-            if (batch, rows, cols) != (q.batch, q.rows, q.cols):
-                raise ValueError(f"out {i} must have its update's order of rows and columns")
+            *_, q.ld_out, q.batch_stride_out = _matrix(outs[i], (q.batch, q.rows, q.cols))
             q.out = outs[i].data_ptr()
     return mats
 

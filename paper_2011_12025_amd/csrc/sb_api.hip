@@ -10,6 +10,7 @@
 
 #include <algorithm>
 #include <mutex>
+#include <new>
 #include <string>
 #include <vector>
 
@@ -1203,7 +1204,7 @@ int check_matrices(const char* fn, const sb_matrix* mats, int count, int dtype, 
 }  // namespace
 
 int segblocks_orthogonalize(const sb_matrix* matrices, int count, int dtype, int steps, const double* coefficients,
-                            double eps, void* workspace, size_t ws_bytes, hipStream_t stream) {
+                            double eps, void* workspace, size_t ws_bytes, hipStream_t stream) try {
     const char* fn = "segblocks_orthogonalize";
     std::vector<sb::OrthMat> v;
     int s;
@@ -1227,9 +1228,12 @@ int segblocks_orthogonalize(const sb_matrix* matrices, int count, int dtype, int
     if (any_overlap(outs, ins)) return fail(SB_EINVAL, fn, "outputs or the workspace overlap inputs or each other");
     return hip_status(fn, sb::launch_orth(dtype, v.data(), count, steps, coefficients, eps, sb::Ws{workspace, need},
                                           stream));
+} catch (const std::bad_alloc&) {  // (the lists above, on the host)
+    g_err.clear();
+    return SB_ENOMEM;
 }
 
-int segblocks_orthogonalize_workspace_size(const sb_matrix* matrices, int count, int dtype, size_t* bytes) {
+int segblocks_orthogonalize_workspace_size(const sb_matrix* matrices, int count, int dtype, size_t* bytes) try {
     const char* fn = "segblocks_orthogonalize_workspace_size";
     std::vector<sb::OrthMat> v;
     int s;
@@ -1238,6 +1242,9 @@ int segblocks_orthogonalize_workspace_size(const sb_matrix* matrices, int count,
     *bytes = sb::orth_ws_bytes(dtype, v.data(), count);
     g_err.clear();
     return SB_OK;
+} catch (const std::bad_alloc&) {
+    g_err.clear();
+    return SB_ENOMEM;
 }
 
 }  // extern "C"

@@ -164,18 +164,25 @@ __global__ __launch_bounds__(WG) void k_orth_amax(Table tb) {
     // rows of vectors, or one row of all where nothing lies between them
     const bool flat = q.ld == q.n;
     const long long cols = flat ? (long long)q.m * q.n : q.n, rows = flat ? 1 : q.m;
-    const long long nv = q.vec & 1 ? cols / V : 0, all = (long long)wgs * WG;
-    for (long long r = 0; r < rows; ++r) {
+    const bool vec = q.vec & 1;
+    const int width = WG * 2 * (vec ? V : 1);  // of a piece of a row: two loads a thread
+    const long long across = (cols + width - 1) / width;
+    for (long long x = p.t; x < rows * across; x += wgs) {
+        const long long r = x / across, c0 = (x - r * across) * width;
         const T* row = g + r * q.ld;
-#pragma unroll 4
-        for (long long v = (long long)p.t * WG + tid; v < nv; v += all) {
-            Vec<T, V> x;
-            x.raw = *reinterpret_cast<const uint4*>(row + v * V);
 #pragma unroll
-            for (int i = 0; i < V; ++i) m = fmaxf(m, fabsf(to_f32(x.e[i])));
+        for (int i = 0; i < 2; ++i) {
+            const long long c = c0 + (i * WG + tid) * (vec ? V : 1);
+            if (vec && c + V <= cols) {
+                Vec<T, V> y;
+                y.raw = *reinterpret_cast<const uint4*>(row + c);
+#pragma unroll
+                for (int k = 0; k < V; ++k) m = fmaxf(m, fabsf(to_f32(y.e[k])));
+            } else {
+                for (int k = 0; k < (vec ? V : 1); ++k)
+                    if (c + k < cols) m = fmaxf(m, fabsf(to_f32(row[c + k])));
+            }
         }
-#pragma unroll 4
-        for (long long c = nv * V + (long long)p.t * WG + tid; c < cols; c += all) m = fmaxf(m, fabsf(to_f32(row[c])));
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
@@ -828,7 +835,7 @@ struct Group {
 
 long long up(long long n, long long k) { return (n + k - 1) / k * k; }
 
-long long sym_count(const Table& tb, int T) {
+long long sym_count(const Table& tb, int T) {  // tiles of one product
     long long n = 0;
     for (int i = 0; i < tb.count; ++i) {
         const long long t = tb.mat[i].sp / T;
@@ -848,6 +855,23 @@ Cut cut_of(long long n, int most) {
     const int rest = (int)(n % SLOTS);
     const int parts = rest == 0 || n < SLOTS ? 1 : std::min(SLOTS / rest, most);
     return parts > 1 ? Cut{(int)n - rest, parts} : Cut{(int)n, 1};
+}
+
+// X X^T of fewer tiles than SLOTS: the longer side is often much the longer, so
+// units over L of one length, of 256 at least, as many as the chip has slots for.
+// Sets the entries' parts and returns all units.
+long long gram_units(Table& tb, int T) {
+    auto tiles = [&](const OMat& q) { const long long t = q.sp / T; return t * (t + 1) / 2 * q.batch; };
+    long long cells = 0, unit = 0;  // cells: steps of 256 of L
+    for (int i = 0; i < tb.count; ++i) cells += tiles(tb.mat[i]) * (up(tb.mat[i].Lp, 256) / 256);
+    const long long len = std::max(1LL, (cells + SLOTS - 1) / SLOTS);
+    for (int i = 0; i < tb.count; ++i) {
+        OMat& q = tb.mat[i];
+        q.parts = (int)std::max(1LL, up(q.Lp, 256) / 256 / len);
+        q.unit0 = (int)unit;
+        unit += tiles(q) * q.parts;
+    }
+    return unit;
 }
 
 // Tiles of 128 where they give every CU one, else of 64 (and for single tiles).
@@ -896,8 +920,16 @@ std::vector<Group> groups_of(const OrthMat* mats, int count) {
             o.ws_one = up(w_sym(o.sp, o.Lp, SYMS), 256);
             g.bytes += (size_t)(o.ws_one * o.batch);
         }
+        // sums of X X^T and, where a product has a remainder to split, of that
         g.sums = g.bytes;
-        g.bytes += (size_t)2 * SLOTS * 128 * 128 * 4;  // (X X^T: less than SLOTS tiles and SLOTS parts more)
+        const long long n128 = unit == 128 ? sym_count(g.tb, 128) : 0, n64 = sym_count(g.tb, 64);
+        const int T = tile_of(n128, unit == 128);
+        long long cells = gram_units(g.tb, T) * T * T;
+        for (int jobs = 1; jobs <= 2; ++jobs) {
+            const int t = tile_of(n128 * jobs, unit == 128);
+            if ((t == 128 ? n128 : n64) * jobs >= SLOTS) cells = std::max(cells, (long long)SLOTS * t * t);
+        }
+        g.bytes += (size_t)cells * 4;
         v.push_back(g);
     }
     return v;
@@ -986,18 +1018,7 @@ struct Runner {
         s.eps = eps;
         s.tiles = (int)number(tb, tiles);
         if (GRAM && (s.tiles < SLOTS || s.leave)) {
-            // the longer side is often much the longer: units over L of one length,
-            // of 256 at least, as many as the chip has slots for
-            long long cells = 0;  // in steps of 256 of L
-            for (int i = 0; i < tb.count; ++i) cells += (long long)tiles(tb.mat[i]) * tb.mat[i].batch * up(tb.mat[i].Lp, 256) / 256;
-            const long long len = std::max(1LL, (cells + SLOTS - 1) / SLOTS);
-            int unit = 0;
-            for (int i = 0; i < tb.count; ++i) {
-                OMat& q = tb.mat[i];
-                q.parts = (int)std::max(1LL, up(q.Lp, 256) / 256 / len);
-                q.unit0 = unit;
-                unit += tiles(q) * q.batch * q.parts;
-            }
+            gram_units(tb, TILE);
             s.whole = -1;
             run<NT<TILE>>(k_orth_sym<TILE, P, S, GRAM>, number(tb, [&](const OMat& q) { return tiles(q) * q.parts; }), lds, s);
             if (!s.leave)

@@ -229,6 +229,16 @@ def test_zeros_ranks_and_scales(m, n, dtype):
     assert bool(a.isnan().all()) and torch.equal(b, sb.orthogonalize(good))
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_single_rows_columns_and_wide_slices(dtype):
+    gen = torch.Generator().manual_seed(9)
+    big = gradient(600, 900, dtype, gen)
+    updates = [big[:, 5:6].t(), big[7:8], big[:, 3:4], big[3:500, 7:300], big[::3, :100], big.t()[10:70]]
+    for g, o in zip(updates, sb.orthogonalize(updates)):
+        assert o.shape == g.shape
+        near(o, reference(g), TOL[dtype], f"{tuple(g.shape)} of strides {g.stride()}")
+
+
 def test_empty_updates_and_lists():
     assert sb.orthogonalize([]) == []
     assert sb.orthogonalize(torch.empty(0, 5, device="cuda")).shape == (0, 5)

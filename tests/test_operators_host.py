@@ -140,6 +140,11 @@ def test_updates_are_read_as_they_lie():
     assert sb._matrix(torch.empty(3, 6, 10)[:, :4]) == (3, 4, 10, 10, 60)
     assert sb._matrix(torch.empty(4, 5, 3, 3)) == (1, 4, 45, 45, 0)
     assert sb._matrix(torch.empty(4, 5, 3, 3).contiguous(memory_format=torch.channels_last)) == (1, 4, 45, 45, 0)
+    # a single row of a column-major slice, and the dense row that it is written to
+    row = m[:, :1].t()
+    assert sb._matrix(row) == (1, 6, 1, 10, 0) and sb._matrix(torch.empty_like(row), (1, 6, 1)) == (1, 6, 1, 1, 0)
+    with pytest.raises(ValueError, match="order of rows"):
+        sb._matrix(torch.empty(6, 10), (1, 10, 6))
     for bad in (m[:, ::2], torch.empty(5), m[:1].expand(4, 10), torch.empty(4, 5, 3, 3)[:, :3]):
         with pytest.raises(ValueError):
             sb._matrix(bad)
