@@ -165,23 +165,20 @@ __global__ __launch_bounds__(WG) void k_orth_amax(Table tb) {
     const bool flat = q.ld == q.n;
     const long long cols = flat ? (long long)q.m * q.n : q.n, rows = flat ? 1 : q.m;
     const bool vec = q.vec & 1;
-    const int width = WG * 2 * (vec ? V : 1);  // of a piece of a row: two loads a thread
-    const long long across = (cols + width - 1) / width;
-    for (long long x = p.t; x < rows * across; x += wgs) {
-        const long long r = x / across, c0 = (x - r * across) * width;
-        const T* row = g + r * q.ld;
+    const int step = vec ? V : 1;
+    const long long across = (cols + step - 1) / step, count = rows * across, all = (long long)wgs * WG;
+#pragma unroll 4
+    for (long long x = (long long)p.t * WG + tid; x < count; x += all) {
+        const long long r = flat ? 0 : x / across, c = (x - r * across) * step;
+        const T* from = g + r * q.ld + c;
+        if (vec && c + V <= cols) {
+            Vec<T, V> y;
+            y.raw = *reinterpret_cast<const uint4*>(from);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const long long c = c0 + (i * WG + tid) * (vec ? V : 1);
-            if (vec && c + V <= cols) {
-                Vec<T, V> y;
-                y.raw = *reinterpret_cast<const uint4*>(row + c);
-#pragma unroll
-                for (int k = 0; k < V; ++k) m = fmaxf(m, fabsf(to_f32(y.e[k])));
-            } else {
-                for (int k = 0; k < (vec ? V : 1); ++k)
-                    if (c + k < cols) m = fmaxf(m, fabsf(to_f32(row[c + k])));
-            }
+            for (int k = 0; k < V; ++k) m = fmaxf(m, fabsf(to_f32(y.e[k])));
+        } else {
+            for (int k = 0; k < step; ++k)
+                if (c + k < cols) m = fmaxf(m, fabsf(to_f32(from[k])));
         }
     }
 #pragma unroll
