@@ -101,15 +101,21 @@ __host__ __device__ inline int prep_wgs(const OMat& q) {
 }
 
 // ---------------------------------------------------------------------------
-// Storage of a matrix of pairs: a row is [k / 32][32 hi | 32 lo]; of single
-// numbers: [k].  NP: numbers an element.
+// Storage of a matrix (S), rows of one of
+//   ONES     [k], single numbers
+//   PAIRS    [k / 32][32 hi | 32 lo], for products that take both
+//   HI_PAIRS [k / 64][64 hi | 64 lo], for products that take hi alone
+// so that a product's step reads whole lines of 128 bytes.
 // ---------------------------------------------------------------------------
-template <int NP>
+enum { ONES = 1, PAIRS = 2, HI_PAIRS = 3 };
+template <int S> constexpr int BYTES = S == ONES ? 2 : 4;           // of an element
+template <int S> constexpr int LO_AT = S == HI_PAIRS ? 128 : 64;    // from hi to lo
+template <int S>
 __device__ __forceinline__ long long at_k(long long k) {  // bytes, k a multiple of 8
-    return NP == 2 ? (k >> 5) * 128 + (k & 31) * 2 : k * 2;
+    return S == ONES ? k * 2 : S == PAIRS ? (k >> 5) * 128 + (k & 31) * 2 : (k >> 6) * 256 + (k & 63) * 2;
 }
 
-template <int NP>
+template <int S>
 __device__ __forceinline__ void store8(char* row, long long k, const float (&v)[8]) {
     Vec<f16, 8> hi, lo;
 #pragma unroll
@@ -123,9 +129,9 @@ __device__ __forceinline__ void store8(char* row, long long k, const float (&v)[
         hi.e[i] = (f16)x;
         lo.e[i] = (f16)(x - (float)hi.e[i]);
     }
-    char* p = row + at_k<NP>(k);
+    char* p = row + at_k<S>(k);
     vstore<f16, 8>((f16*)p, hi);
-    if (NP == 2) vstore<f16, 8>((f16*)(p + 64), lo);
+    if (S != ONES) vstore<f16, 8>((f16*)(p + LO_AT<S>), lo);
 }
 
 // An R x T piece in LDS (fp32, rows CP<T> apart) to rows r0.. and columns c0.. of a
@@ -137,7 +143,7 @@ template <int T> constexpr int CP = T + 1;
 // have two, each with half of a stage's K (s = 512: 12.4 -> 11.0 us a product).
 template <int T> constexpr int NT = T == 64 ? 512 : 256;
 
-template <int T, int NP, bool TURNED, int R = T, int THREADS = NT<T>>
+template <int T, int S, bool TURNED, int R = T, int THREADS = NT<T>>
 __device__ __forceinline__ void store_tile(const float* C, char* dst, long long K, int r0, int c0) {
     constexpr int W = (TURNED ? R : T) / 8;  // eights of a stored row
     for (int e = (int)threadIdx.x; e < R * T / 8; e += THREADS) {
@@ -145,7 +151,7 @@ __device__ __forceinline__ void store_tile(const float* C, char* dst, long long 
         float v[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = TURNED ? C[(k + i) * CP<T> + r] : C[r * CP<T> + k + i];
-        store8<NP>(dst + (long long)(r0 + r) * K * (2 * NP), c0 + k, v);
+        store8<S>(dst + (long long)(r0 + r) * K * BYTES<S>, c0 + k, v);
     }
 }
 
@@ -224,7 +230,7 @@ __device__ __forceinline__ float norm_factor(const OMat& q, const char* ws, floa
 // X [sp][Lp] and its transpose [Lp][sp] from the update, and its squares.
 template <typename T>
 __global__ __launch_bounds__(WG) void k_orth_prep(Table tb) {
-    constexpr int NP = sizeof(T) == 4 ? 2 : 1, V = 16 / (int)sizeof(T);
+    constexpr int S = sizeof(T) == 4 ? PAIRS : ONES, V = 16 / (int)sizeof(T);
     __shared__ float C[64 * CP<64>];
     __shared__ float s4[WG / 64];
     const Place p = place(tb, [](const OMat& q) { return prep_wgs(q); }, (int)blockIdx.x);
@@ -267,8 +273,8 @@ __global__ __launch_bounds__(WG) void k_orth_prep(Table tb) {
             }
         }
         __syncthreads();
-        store_tile<64, NP, false, 64, WG>(C, tall ? Xt : X, np, r0, c0);
-        store_tile<64, NP, true, 64, WG>(C, tall ? X : Xt, mp, c0, r0);
+        store_tile<64, S, false, 64, WG>(C, tall ? Xt : X, np, r0, c0);
+        store_tile<64, S, true, 64, WG>(C, tall ? X : Xt, mp, c0, r0);
         __syncthreads();
     }
 #pragma unroll
@@ -279,25 +285,26 @@ __global__ __launch_bounds__(WG) void k_orth_prep(Table tb) {
 }
 
 // ---------------------------------------------------------------------------
-// A T x T tile of A B^T, K in steps of 32: both operands' rows go to LDS by DMA
-// (16 bytes a lane) while the steps before are multiplied.  128 (64) bytes a row
-// and step, its 16-byte chunks XORed by the pair (four) of rows, so that 16 rows
-// lie in distinct ones of the 64 banks (XORed by the row, with 8 distinct, a read
-// took twice the cycles).  Four waves, each a quarter of
-// the tile in v_mfma_f32_32x32x16_f16.
+// A T x T tile of A B^T, K in steps of 32 (of 64 where both operands are single
+// numbers): both operands' rows go to LDS by DMA (16 bytes a lane) while the steps
+// before are multiplied.  128 (64) bytes a row and step, its 16-byte chunks XORed by
+// the pair (four) of rows, so that 16 rows lie in distinct ones of the 64 banks
+// (XORed by the row, with 8 distinct, a read took twice the cycles).  Four waves,
+// each a quarter of the tile in v_mfma_f32_32x32x16_f16.
 // ---------------------------------------------------------------------------
 template <int T> constexpr int MF = T / 64;  // 32 x 32 fragments of a wave, each way
 
-template <int NP>
+template <int BYTES_ROW>
 __device__ __forceinline__ int chunk_of(int row, int c) {  // where chunk c of a row lies
-    return NP == 2 ? c ^ ((row >> 1) & 7) : c ^ ((row >> 2) & 3);
+    return BYTES_ROW == 128 ? c ^ ((row >> 1) & 7) : c ^ ((row >> 2) & 3);
 }
 
 // Steps of 32 that a stage holds, and the elements of K of one: with tiles of 64 the
 // latency of a stage (LDS reads, then the chain of MFMAs) counts, so it is longer.
+// Products of single numbers take 64 elements in either.
 template <int T> constexpr int KS = T == 64 ? 2 : 1;
-template <int T> constexpr __host__ __device__ int step_k() { return 32 * KS<T>; }
-template <int T, int NA, int NB> constexpr int stage_bytes() { return T * 64 * KS<T> * (NA + NB); }
+template <int T, int NA, int NB> constexpr int STEP_K = NA + NB == 2 ? 64 : 32 * KS<T>;
+template <int T, int NA, int NB> constexpr int stage_bytes() { return T * 2 * STEP_K<T, NA, NB> * (NA + NB); }
 // Stages in LDS.  Tiles of 128: as many as leave room for two workgroups on a CU.
 // Tiles of 64 are for products that do not fill the chip: one workgroup a CU,
 // and what it has in flight against the latency of another XCD's results decides.
@@ -329,7 +336,7 @@ __device__ __forceinline__ void dma16(const char* from, unsigned char* to) {
 }
 
 // rows of A and B from their first element on; the tile ends in LDS as fp32.  NA,
-// NB: numbers of an element that take part, SA, SB: that are stored (1 of 2: hi).
+// NB: numbers of an element that take part, SA, SB: how they are stored.
 //
 // A wave's DMA instructions are spread over its MFMAs: a CU takes one (1 KB) in
 // about 28 cycles, and a wave that issues a stage's eight in a row stands still
@@ -337,32 +344,42 @@ __device__ __forceinline__ void dma16(const char* from, unsigned char* to) {
 // 100 us, MFMAs with their LDS reads alone 112, together 207 and spread 196 (1.08
 // PFLOP/s of MFMA, where a large library product reaches 1.21).  More stages (one
 // workgroup of eight waves a CU), or operands read a stage ahead, were no faster.
-template <int T, int NA, int NB, int SA = NA, int SB_ = NB>
+template <int T, int NA, int NB, int SA, int SB>
 __device__ __forceinline__ void product_tile(const char* A, long long pa, const char* B, long long pb, int step0,
                                              int steps, unsigned char* lds) {
-    constexpr int SB = stage_bytes<T, NA, NB>(), HB = T * 64 * (NA + NB), OB = T * 64 * NA, NST = stages<T, NA, NB>();
-    // DMA instructions of a group of four waves and step of 32; of a wave and stage
-    constexpr int LA = T * 4 * NA / WG, LB = T * 4 * NB / WG, LH = LA + LB, GROUPS = NT<T> / WG;
-    constexpr int LOADS = KS<T> * LH / GROUPS;
-    static_assert(KS<T> % GROUPS == 0, "a group takes whole steps of 32");
+    constexpr bool ONE = NA + NB == 2;
+    static_assert(ONE || (SA == NA && SB == NB), "steps of 32 of what is stored");
+    constexpr int RA = ONE ? 128 : 64 * NA, RB = ONE ? 128 : 64 * NB;  // bytes of a row and step
+    constexpr int STAGE = stage_bytes<T, NA, NB>(), OB = T * RA, STEP = T * (RA + RB), NST = stages<T, NA, NB>();
+    // Two groups of four waves take steps of 32 in turn, or halves of one step of 64.
+    constexpr int GROUPS = NT<T> / WG, LOADERS = ONE ? NT<T> : WG, STEPS = ONE ? 1 : KS<T>;
+    // DMA instructions of a thread and step; of a thread and stage
+    constexpr int LA = T * RA / 16 / LOADERS, LB = T * RB / 16 / LOADERS, LH = LA + LB;
+    constexpr int LOADS = ONE ? LH : STEPS * LH / GROUPS;
+    static_assert(ONE || STEPS % GROUPS == 0, "a group takes whole steps of 32");
+    // bytes that a step takes along a stored row
+    constexpr long long GA = ONE ? 64 * BYTES<SA> : RA, GB = ONE ? 64 * BYTES<SB> : RB;
     // the three products of a 64 x 64 tile's one fragment in sums of their own:
     // an MFMA waits for the one before it on the same sum
     constexpr int CH = T == 64 ? NA + NB - 1 : 1;
-    const int tid = (int)threadIdx.x & (WG - 1), l = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int tid = (int)threadIdx.x & (LOADERS - 1), l = lane_id();
+    const int wave = __builtin_amdgcn_readfirstlane(((int)threadIdx.x & (WG - 1)) >> 6);
+    const int loader = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int group = GROUPS == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x / WG);
     const int ra = (wave >> 1) * (T / 2) + (l & 31), rb = (wave & 1) * (T / 2) + (l & 31);
     // this lane's 16 bytes of every instruction, from the operand's first row
     unsigned from[LH];
 #pragma unroll
     for (int i = 0; i < LH; ++i) {
-        const int np = i < LA ? NA : NB, c = (i < LA ? i : i - LA) * WG + tid, r = c / (4 * np);
-        const int chunk = i < LA ? chunk_of<NA>(r, c % (4 * NA)) : chunk_of<NB>(r, c % (4 * NB));
+        const int chunks = (i < LA ? RA : RB) / 16, c = (i < LA ? i : i - LA) * LOADERS + tid, r = c / chunks;
+        const int chunk = i < LA ? chunk_of<RA>(r, c % chunks) : chunk_of<RB>(r, c % chunks);
         from[i] = (unsigned)(r * (i < LA ? pa : pb) + chunk * 16);
     }
     auto dma = [&](int i, int s, int buf) {  // instruction i of stage s
-        const int k = i / LH * GROUPS + group, j = i % LH;
-        const char* base = (j < LA ? A : B) + ((long long)(step0 + s) * KS<T> + k) * (64 * (j < LA ? SA : SB_));
-        unsigned char* to = lds + buf * SB + k * HB + (j < LA ? j : j - LA) * (WG * 16) + (j < LA ? 0 : OB) + wave * 1024;
+        const int k = ONE ? 0 : i / LH * GROUPS + group, j = i % LH;
+        const char* base = (j < LA ? A : B) + ((long long)(step0 + s) * STEPS + k) * (j < LA ? GA : GB);
+        unsigned char* to = lds + buf * STAGE + k * STEP + (j < LA ? j : j - LA) * (LOADERS * 16) + (j < LA ? 0 : OB) +
+                            loader * 1024;
         dma16(base + from[j], to);
     };
     floatx16 acc[CH][MF<T>][MF<T>] = {};
@@ -373,25 +390,25 @@ __device__ __forceinline__ void product_tile(const char* A, long long pa, const 
     for (int s = 0; s < steps; ++s) {
         if (s + NST - 2 < steps) product_barrier<(NST - 2) * LOADS>();
         else product_barrier<0>();
-        const unsigned char* cur = lds + at * SB;
+        const unsigned char* cur = lds + at * STAGE;
         const bool more = s + NST - 1 < steps;
         const int into = at == 0 ? NST - 1 : at - 1;
         at = at + 1 == NST ? 0 : at + 1;
-        constexpr int J = 2 * KS<T> / GROUPS;
+        constexpr int J = STEP_K<T, NA, NB> / 16 / GROUPS;
         halfx8 fa[J][NA][MF<T>], fb[J][NB][MF<T>];  // of the whole stage: their reads are in flight together
 #pragma unroll
         for (int j = 0; j < J; ++j) {
-            const int c = 2 * (j & 1) + (l >> 5);
-            const unsigned char* half = cur + ((j >> 1) * GROUPS + group) * HB;
+            const int c = (ONE ? 2 * (J * group + j) : 2 * (j & 1)) + (l >> 5);
+            const unsigned char* step = cur + (ONE ? 0 : ((j >> 1) * GROUPS + group) * STEP);
 #pragma unroll
             for (int i = 0; i < MF<T>; ++i) {
 #pragma unroll
                 for (int h = 0; h < NA; ++h)
-                    fa[j][h][i] = *(const halfx8*)(half + (ra + 32 * i) * (64 * NA) + chunk_of<NA>(ra + 32 * i, 4 * h + c) * 16);
+                    fa[j][h][i] = *(const halfx8*)(step + (ra + 32 * i) * RA + chunk_of<RA>(ra + 32 * i, 4 * h + c) * 16);
 #pragma unroll
                 for (int h = 0; h < NB; ++h)
-                    fb[j][h][i] = *(const halfx8*)(half + OB + (rb + 32 * i) * (64 * NB) +
-                                                   chunk_of<NB>(rb + 32 * i, 4 * h + c) * 16);
+                    fb[j][h][i] = *(const halfx8*)(step + OB + (rb + 32 * i) * RB +
+                                                   chunk_of<RB>(rb + 32 * i, 4 * h + c) * 16);
             }
         }
         constexpr int MM = J * (NA + NB - 1) * MF<T> * MF<T>;  // MFMAs of a stage
@@ -470,32 +487,30 @@ __device__ __forceinline__ void sym_tile(int t, int n, int& bi, int& bj) {
 
 // out = alpha C + beta D + gamma I for R x T cells at (r0, c0) of symmetric
 // matrices [sp][sp], and their mirror image.
-template <int T, int R>
+template <int T, int R, int S>
 __device__ __forceinline__ void store_sym(float* C, char* out, const char* D, int sp, int r0, int c0, bool mirror,
-                                          bool one, float alpha, float beta, float gamma) {
+                                          float alpha, float beta, float gamma) {
     for (int e = (int)threadIdx.x; e < R * T / 8; e += NT<T>) {
         const int r = e / (T / 8), k = (e % (T / 8)) * 8, K = c0 + k;
-        const long long row = (long long)(r0 + r) * sp * 4;
+        const long long row = (long long)(r0 + r) * sp * BYTES<S>;
         float v[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = alpha * C[r * CP<T> + k + i];
         if (D) {
-            const Vec<f16, 8> hi = vload<f16, 8>((const f16*)(D + row + at_k<2>(K)));
-            const Vec<f16, 8> lo = vload<f16, 8>((const f16*)(D + row + at_k<2>(K) + 64));
+            const Vec<f16, 8> hi = vload<f16, 8>((const f16*)(D + row + at_k<S>(K)));
+            Vec<f16, 8> lo = vzero<f16, 8>();
+            if (S != ONES) lo = vload<f16, 8>((const f16*)(D + row + at_k<S>(K) + LO_AT<S>));
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 v[i] += beta * ((float)hi.e[i] + (float)lo.e[i]) + (r0 + r == K + i ? gamma : 0.0f);
         }
-        if (one)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = (float)(f16)v[i];
-        store8<2>(out + row, K, v);
+        store8<S>(out + row, K, v);
 #pragma unroll
         for (int i = 0; i < 8; ++i) C[r * CP<T> + k + i] = v[i];
     }
     if (!mirror) return;
     __syncthreads();
-    store_tile<T, 2, true, R>(C, out, sp, c0, r0);
+    store_tile<T, S, true, R>(C, out, sp, c0, r0);
 }
 
 // One or two products that give symmetric matrices (numbers of the
@@ -515,7 +530,6 @@ struct SymLaunch {
     int whole, parts, first;
     int x;      // of X X^T: which X
     int leave;  // sums of every tile, for k_orth_steps
-    int one;    // the result rounded to one fp16 number (its lo is 0)
     float eps;
     float* sums;  // [unit][T * T], units counted from the first split tile's (whole < 0: from the first of all)
 };
@@ -540,7 +554,7 @@ __device__ __forceinline__ SymUnit sym_unit(const Table& tb, const SymLaunch& s,
 }
 
 // C: R rows of the tile from row `part` R on.
-template <int T, int R, bool GRAM>
+template <int T, int R, int O, bool GRAM>
 __device__ __forceinline__ void sym_out(const OMat& q, char* ws, const SymLaunch& s, const SymJob& j, int t, int part,
                                         float* C) {
     int bi, bj;
@@ -551,11 +565,11 @@ __device__ __forceinline__ void sym_out(const OMat& q, char* ws, const SymLaunch
         const float f = norm_factor(q, ws, s.eps);
         alpha *= f * f;
     }
-    store_sym<T, R>(C, sym(j.c), GRAM || j.d < 0 ? nullptr : sym(j.d), q.sp, bi * T + part * R, bj * T, bi != bj,
-                    s.one, alpha, j.beta, j.gamma);
+    store_sym<T, R, O>(C, sym(j.c), GRAM || j.d < 0 ? nullptr : sym(j.d), q.sp, bi * T + part * R, bj * T, bi != bj,
+                       alpha, j.beta, j.gamma);
 }
 
-template <int T, int NP, int S, bool GRAM>  // NP of the S stored numbers of an element
+template <int T, int NP, int S, int O, bool GRAM>  // NP numbers of what is stored as S take part; O: how the result is
 __global__ __launch_bounds__(NT<T>, 2) void k_orth_sym(Table tb, SymLaunch s) {
     extern __shared__ __align__(16) unsigned char lds[];
     const SymUnit u = sym_unit<T>(tb, s, (int)blockIdx.x);
@@ -564,9 +578,9 @@ __global__ __launch_bounds__(NT<T>, 2) void k_orth_sym(Table tb, SymLaunch s) {
     char* ws = q.ws + u.p.b * q.ws_one;
     int bi, bj;
     sym_tile(u.p.t, q.sp / T, bi, bj);
-    const int K = GRAM ? q.Lp : q.sp, steps = K / step_k<T>();
+    const int K = GRAM ? q.Lp : q.sp, steps = K / STEP_K<T, NP, NP>;
     const int k0 = (int)((long long)steps * u.part / u.parts), k1 = (int)((long long)steps * (u.part + 1) / u.parts);
-    const long long pitch = (long long)K * (2 * S);
+    const long long pitch = (long long)K * BYTES<S>;
     const char* A = GRAM ? ws + w_x(q.sp, q.Lp, s.x) : ws + w_sym(q.sp, q.Lp, j.a);
     const char* B = GRAM ? A : ws + w_sym(q.sp, q.Lp, j.b);
     product_tile<T, NP, NP, S, S>(A + bi * T * pitch, pitch, B + bj * T * pitch, pitch, k0, k1 - k0, lds);
@@ -579,12 +593,12 @@ __global__ __launch_bounds__(NT<T>, 2) void k_orth_sym(Table tb, SymLaunch s) {
         }
         return;
     }
-    sym_out<T, T, GRAM>(q, ws, s, j, u.p.t, 0, C);
+    sym_out<T, T, O, GRAM>(q, ws, s, j, u.p.t, 0, C);
 }
 
 // The parts of the split tiles added in their order, a few rows a workgroup.
 template <int T> constexpr int JOIN_ROWS = T == 64 ? 32 : 16;
-template <int T, bool GRAM>
+template <int T, int O, bool GRAM>
 __global__ __launch_bounds__(NT<T>) void k_orth_join(Table tb, SymLaunch s) {
     constexpr int R = JOIN_ROWS<T>, N = R * T / 4 / NT<T>;  // vectors of a thread
     __shared__ float C[R * CP<T>];
@@ -622,7 +636,7 @@ __global__ __launch_bounds__(NT<T>) void k_orth_join(Table tb, SymLaunch s) {
         c[3] = sum[i].w;
     }
     __syncthreads();
-    sym_out<T, R, GRAM>(q, q.ws + u.p.b * q.ws_one, s, s.job[u.job], u.p.t, slice, C);
+    sym_out<T, R, O, GRAM>(q, q.ws + u.p.b * q.ws_one, s, s.job[u.job], u.p.t, slice, C);
 }
 
 // A block of steps on matrices of one tile (s <= 64) without leaving a workgroup:
@@ -642,7 +656,7 @@ constexpr int STEPS_LDS = 5 * 64 * 256;
 
 // Where 8 elements k.. of a row lie in a matrix in LDS (the hi part; lo is chunk + 4).
 __device__ __forceinline__ int step_at(int row, int k, bool lo) {
-    return (k >> 5) * (64 * 128) + row * 128 + chunk_of<2>(row, (k >> 3 & 3) + (lo ? 4 : 0)) * 16;
+    return (k >> 5) * (64 * 128) + row * 128 + chunk_of<128>(row, (k >> 3 & 3) + (lo ? 4 : 0)) * 16;
 }
 
 // c = alpha (a b^T)^T + beta d + gamma I by four waves (d nullptr: the product
@@ -752,7 +766,7 @@ __global__ __launch_bounds__(512) void k_orth_steps(Table tb, Steps st) {
 
 // Q X: the next block's X and its transpose, or the result.  DIRECT: the single
 // step a X + B X instead, Q being B, where both factors of the product are their
-// hi alone and a X has what X has.  S: stored numbers of an element of X.
+// hi alone (B is stored as that) and a X has what X has.  S: how X is stored.
 struct Apply {
     int Q, xt, first;
     float alpha, a, eps;  // alpha Q X + a X
@@ -760,28 +774,29 @@ struct Apply {
 template <int T, int S, typename TO, bool LAST, bool DIRECT>
 __global__ __launch_bounds__(NT<T>, 2) void k_orth_apply(Table tb, Apply ap) {
     extern __shared__ __align__(16) unsigned char lds[];
-    constexpr int NQ = DIRECT ? 1 : 2, NX = DIRECT ? 1 : S;
+    constexpr int NQ = DIRECT ? 1 : 2, NX = DIRECT ? 1 : S, SQ = DIRECT ? ONES : PAIRS;
     const Place p = place(tb, [](const OMat& q) { return (q.sp / T) * (q.Lp / T); }, (int)blockIdx.x);
     const OMat& q = tb.mat[p.mat];
     char* ws = q.ws + p.b * q.ws_one;
     // strips of eight rows of Q, each along L
     const int strip = p.t / (8 * (q.Lp / T)), h = min(8, q.sp / T - 8 * strip), local = p.t - strip * (8 * (q.Lp / T));
     const int k = local / h, i = 8 * strip + (local - k * h);
-    const long long pq = (long long)q.sp * 4, px = (long long)q.sp * (2 * S);
+    const long long pq = (long long)q.sp * BYTES<SQ>, px = (long long)q.sp * BYTES<S>;
     const char* X = ws + w_x(q.sp, q.Lp, ap.xt);
     const char* Xt = ws + w_xt(q.sp, q.Lp, ap.xt);
     const char* qm = ws + w_sym(q.sp, q.Lp, ap.Q) + i * T * pq;
     const char* xm = Xt + k * T * px;
     const bool tall = LAST && q.m > q.n;  // then the tile's rows are those of Xt
-    if (tall) product_tile<T, NX, NQ, S, 2>(xm, px, qm, pq, 0, q.sp / step_k<T>(), lds);
-    else product_tile<T, NQ, NX, 2, S>(qm, pq, xm, px, 0, q.sp / step_k<T>(), lds);
+    const int steps = q.sp / STEP_K<T, NQ, NX>;
+    if (tall) product_tile<T, NX, NQ, S, SQ>(xm, px, qm, pq, 0, steps, lds);
+    else product_tile<T, NQ, NX, SQ, S>(qm, pq, xm, px, 0, steps, lds);
     float* C = (float*)lds;
     const float f = ap.first ? norm_factor(q, ws, ap.eps) : 1.0f;
     {  // each thread its own eights
         const float alpha = f * ap.alpha, a = f * ap.a;
         const char* D = tall ? Xt : X;
         const int r0 = (tall ? k : i) * T, c0 = (tall ? i : k) * T;
-        const long long pd = (long long)(tall ? q.sp : q.Lp) * (2 * S);
+        const long long pd = (long long)(tall ? q.sp : q.Lp) * BYTES<S>;
         for (int e = (int)threadIdx.x; e < T * T / 8; e += NT<T>) {
             const int r = e / (T / 8), c = (e % (T / 8)) * 8;
             float* v = C + r * CP<T> + c;
@@ -789,7 +804,7 @@ __global__ __launch_bounds__(NT<T>, 2) void k_orth_apply(Table tb, Apply ap) {
                 const char* d = D + (r0 + r) * pd + at_k<S>(c0 + c);
                 const Vec<f16, 8> hi = vload<f16, 8>((const f16*)d);
                 Vec<f16, 8> lo = vzero<f16, 8>();
-                if (S == 2) lo = vload<f16, 8>((const f16*)(d + 64));
+                if (S != ONES) lo = vload<f16, 8>((const f16*)(d + LO_AT<S>));
 #pragma unroll
                 for (int x = 0; x < 8; ++x) v[x] = alpha * v[x] + a * ((float)hi.e[x] + (float)lo.e[x]);
             } else {
@@ -816,8 +831,9 @@ __global__ __launch_bounds__(NT<T>, 2) void k_orth_apply(Table tb, Apply ap) {
                     if (c + n < q.n) to[n] = v.e[n];
         }
     } else {
-        store_tile<T, 2, false>(C, ws + w_x(q.sp, q.Lp, ap.xt ^ 1), q.Lp, i * T, k * T);
-        store_tile<T, 2, true>(C, ws + w_xt(q.sp, q.Lp, ap.xt ^ 1), q.sp, k * T, i * T);
+        constexpr int O = DIRECT ? HI_PAIRS : PAIRS;
+        store_tile<T, O, false>(C, ws + w_x(q.sp, q.Lp, ap.xt ^ 1), q.Lp, i * T, k * T);
+        store_tile<T, O, true>(C, ws + w_xt(q.sp, q.Lp, ap.xt ^ 1), q.sp, k * T, i * T);
     }
 }
 
@@ -978,7 +994,7 @@ float pow2(int e) { return (float)ldexp(1.0, std::max(-140, std::min(120, e))); 
 
 template <typename T>
 struct Runner {
-    static constexpr int NP = sizeof(T) == 4 ? 2 : 1;
+    static constexpr int NP = sizeof(T) == 4 ? 2 : 1;  // numbers of an element of the first X, and its storage
     // (see the head of this file)
     static constexpr double MAX_GROWTH = std::is_same<T, bf16>::value ? 2.1e4 : std::is_same<T, f16>::value ? 150.0 : 12.5;
     Table& tb;
@@ -1007,7 +1023,7 @@ struct Runner {
         err = hipGetLastError();
     }
 
-    template <int TILE, int P, int S, bool GRAM>
+    template <int TILE, int P, int S, int O, bool GRAM>
     void sym_t(SymLaunch& s, int jobs) {
         constexpr int lds = product_lds<TILE, P, P>(), SLICES = TILE / JOIN_ROWS<TILE>;
         auto tiles = [](const OMat& q) { const int t = q.sp / TILE; return t * (t + 1) / 2; };
@@ -1017,9 +1033,9 @@ struct Runner {
         if (GRAM && (s.tiles < SLOTS || s.leave)) {
             gram_units(tb, TILE);
             s.whole = -1;
-            run<NT<TILE>>(k_orth_sym<TILE, P, S, GRAM>, number(tb, [&](const OMat& q) { return tiles(q) * q.parts; }), lds, s);
+            run<NT<TILE>>(k_orth_sym<TILE, P, S, O, GRAM>, number(tb, [&](const OMat& q) { return tiles(q) * q.parts; }), lds, s);
             if (!s.leave)
-                run<NT<TILE>>(k_orth_join<TILE, GRAM>,
+                run<NT<TILE>>(k_orth_join<TILE, O, GRAM>,
                               number(tb, [&](const OMat& q) { return q.parts > 1 ? tiles(q) * SLICES : 0; }), 0, s);
             return;
         }
@@ -1027,16 +1043,16 @@ struct Runner {
         s.whole = c.whole;
         s.parts = c.parts;
         const int rest = s.tiles * jobs - c.whole;
-        run<NT<TILE>>(k_orth_sym<TILE, P, S, GRAM>, (unsigned)(c.whole + rest * c.parts), lds, s);
-        if (rest) run<NT<TILE>>(k_orth_join<TILE, GRAM>, (unsigned)(rest * SLICES), 0, s);
+        run<NT<TILE>>(k_orth_sym<TILE, P, S, O, GRAM>, (unsigned)(c.whole + rest * c.parts), lds, s);
+        if (rest) run<NT<TILE>>(k_orth_join<TILE, O, GRAM>, (unsigned)(rest * SLICES), 0, s);
     }
-    template <int P, int S, bool GRAM>
+    template <int P, int S, int O, bool GRAM>
     void sym(SymLaunch s, int jobs = 1) {
-        if (tile_of(sym_count(tb, 128) * jobs, wide) == 128) sym_t<128, P, S, GRAM>(s, jobs);
-        else sym_t<64, P, S, GRAM>(s, jobs);
+        if (tile_of(sym_count(tb, 128) * jobs, wide) == 128) sym_t<128, P, S, O, GRAM>(s, jobs);
+        else sym_t<64, P, S, O, GRAM>(s, jobs);
     }
-    void products(const SymJob& a) { sym<2, 2, false>(SymLaunch{{a, a}}); }
-    void products(const SymJob& a, const SymJob& b) { sym<2, 2, false>(SymLaunch{{a, b}}, 2); }
+    void products(const SymJob& a) { sym<2, PAIRS, PAIRS, false>(SymLaunch{{a, a}}); }
+    void products(const SymJob& a, const SymJob& b) { sym<2, PAIRS, PAIRS, false>(SymLaunch{{a, b}}, 2); }
 
     template <int TILE, int S, bool LAST, bool DIRECT>
     void apply_t(const Apply& ap) {
@@ -1053,8 +1069,9 @@ struct Runner {
     }
     template <bool DIRECT>
     void apply(const Apply& ap, bool last) {
+        constexpr int S = DIRECT ? HI_PAIRS : PAIRS;  // (of X after the first)
         if (ap.first) last ? apply<NP, true, DIRECT>(ap) : apply<NP, false, DIRECT>(ap);
-        else last ? apply<2, true, DIRECT>(ap) : apply<2, false, DIRECT>(ap);
+        else last ? apply<S, true, DIRECT>(ap) : apply<S, false, DIRECT>(ap);
     }
 
     // One step at a time with products of single fp16 numbers, for bf16 alone (the
@@ -1086,12 +1103,10 @@ struct Runner {
             SymLaunch s{{{0, 0, 0, -1, pow2(ea - 2 * ex), 0.0f, 0.0f}, {}}};
             s.first = k == 0;
             s.x = k & 1;
-            s.one = 1;
-            if (k == 0) sym<1, NP, true>(s);
-            else sym<1, 2, true>(s);
+            if (k == 0) sym<1, ONES, ONES, true>(s);
+            else sym<1, HI_PAIRS, ONES, true>(s);
             s = SymLaunch{{{0, 0, 1, 0, (float)(c[2] * pow2(eb - 2 * ea)), (float)(c[1] * pow2(eb - ea)), 0.0f}, {}}};
-            s.one = 1;
-            sym<1, 2, false>(s);
+            sym<1, ONES, ONES, false>(s);
             apply<true>(Apply{1, k & 1, k == 0, pow2(ex2 - eb - ex), (float)(c[0] * pow2(ex2 - ex)), eps}, last);
             lambda = b.lambda;
             ex = ex2;
@@ -1122,8 +1137,8 @@ struct Runner {
             gram.leave = single;
             gram.x = xt;
             Steps list{};
-            if (first) sym<NP, NP, true>(gram);
-            else sym<2, 2, true>(gram);
+            if (first) sym<NP, NP, PAIRS, true>(gram);
+            else sym<2, PAIRS, PAIRS, true>(gram);
             int Q = -1, eq = 0;  // Q: which of the workspace's matrices 2, 3, 4
             double qb = 1.0;
             for (int k = 0; k < len; ++k, ++step) {
