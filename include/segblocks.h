@@ -574,9 +574,12 @@ typedef struct {
  *   a matrix with more rows than columns is taken transposed),
  * written to out in `dtype`.  coefficients: HOST array of a, b, c for every
  * step (3 * steps).  1 <= steps <= 32, eps >= 0; a matrix of zeros gives
- * zeros, one with NaN or an infinity gives NaN.  The sums are fp32; matrices
- * between the products are held to 22 bits or more, so the result is that of
- * an fp32 iteration also for a 16-bit update, rounded once.  Workspace:
+ * zeros, one with NaN or an infinity gives NaN.  The sums are fp32, and
+ * matrices between the products are held to 22 bits and a sign, so the result
+ * is that of an fp32 iteration also for a 16-bit update, rounded once; but
+ * for bf16 with up to five steps, where the sides are not far apart, factors
+ * of products are rounded to 11 bits (fp16), which adds about 1.2e-3 of the
+ * norm to the 1.7e-3 of the result's own rounding.  Workspace:
  * segblocks_orthogonalize_workspace_size (a function of the entries' sizes,
  * pointers not looked at). */
 int segblocks_orthogonalize(const sb_matrix* matrices, int count, int dtype, int steps, const double* coefficients,

@@ -596,30 +596,54 @@ __global__ __launch_bounds__(NW == 1 ? 256 : NW * 64) void k_logp_planes(LogpArg
 // ---------------------------------------------------------------------------
 // Gradient
 // ---------------------------------------------------------------------------
+// Up to K alternatives in registers (class -1: none), which may name a class twice.
+// K = 0: there are none; K < 0: more than that, read where they are needed.
+template <int K>
+struct Alts {
+    int j[K > 0 ? K : 1];
+    float g[K > 0 ? K : 1];
+};
+
 struct GradRow {
     float m, ln_s, g, G, gh, H;
-    long long label;  // -1: none
+    int label;  // -1: none
     bool empty;
 
-    __device__ __forceinline__ GradRow(const LogpGradArgs& a, long long r, long long n, long long p) {
+    template <int K>
+    __device__ __forceinline__ GradRow(const LogpGradArgs& a, long long r, long long n, long long p, Alts<K>& alts) {
         m = a.lse[r];
         ln_s = 0.0f;
         empty = m == -INFINITY;
         g = 0.0f;
         label = -1;
         if (a.d_logp) {
-            label = a.labels[r];
-            if (label == a.ignore) label = -1;
-            else g = label < 0 || label >= a.C ? NAN : a.d_logp[r];
+            const long long l = a.labels[r];
+            const bool in = l >= 0 && l < a.C;
+            if (l != a.ignore) {
+                label = in ? (int)l : -1;
+                g = in ? a.d_logp[r] : NAN;
+            }
         }
         gh = a.d_entropy ? a.d_entropy[r] : 0.0f;
         H = a.d_entropy ? a.entropy[r] : 0.0f;
         G = g;
+        auto take = [&](long long q, int& j, float& d) {
+            j = a.top_index[q];
+            d = a.d_top[q];
+            G += j < 0 || j >= a.C ? NAN : d;
+        };
+        if constexpr (K > 0) {
+#pragma unroll
+            for (int u = 0; u < K; ++u) {
+                alts.j[u] = -1;
+                alts.g[u] = 0.0f;
+                if (u < a.topk) take((n * a.topk + u) * a.P + p, alts.j[u], alts.g[u]);
+            }
+        } else if constexpr (K < 0) {
+            int j;
+            float d;
 #pragma unroll 8
-        for (int i = 0; i < a.topk; ++i) {
-            const long long q = (n * a.topk + i) * a.P + p;
-            const int j = a.top_index[q];
-            G += j < 0 || j >= a.C ? NAN : a.d_top[q];
+            for (int i = 0; i < a.topk; ++i) take((n * a.topk + i) * a.P + p, j, d);
         }
     }
     // p from lse is off by |lse| 2^-25: past 256 it comes from the row's own maximum
@@ -648,6 +672,44 @@ struct GradRow {
         }
         return d;
     }
+    // The same with alternatives in registers (K <= 0: the label alone).
+    template <int K>
+    __device__ __forceinline__ float at(const Alts<K>& alts, float z, int c) const {
+        float d = all(z);
+        if (empty) return d;
+        d += c == label ? g : 0.0f;
+        if constexpr (K > 0)
+#pragma unroll
+            for (int u = 0; u < K; ++u) d += c == alts.j[u] ? alts.g[u] : 0.0f;
+        return d;
+    }
+    // More of them than registers hold, in [c0, c1) by one thread after the rest: eight
+    // at a time against the whole list (each for itself, 20 alternatives of 10000
+    // pixels took 34 us, mostly round trips to the list, and so 21).
+    template <typename Get, typename Put>
+    __device__ __forceinline__ void again(const LogpGradArgs& a, long long n, long long p, int c0, int c1, Get get, Put put) const {
+        if (empty) return;
+        for (int i0 = 0; i0 < a.topk; i0 += 8) {
+            int j[8];
+            float d[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                j[u] = a.top_index[(n * a.topk + min(i0 + u, a.topk - 1)) * a.P + p];  // (the last one again: the same value)
+                d[u] = j[u] == label ? g : 0.0f;
+            }
+#pragma unroll 8
+            for (int i = 0; i < a.topk; ++i) {
+                const long long q = (n * a.topk + i) * a.P + p;
+                const int ji = a.top_index[q];
+                const float gi = a.d_top[q];
+#pragma unroll
+                for (int u = 0; u < 8; ++u) d[u] += ji == j[u] ? gi : 0.0f;
+            }
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                if (j[u] >= c0 && j[u] < c1) put(j[u], all(get(j[u])) + d[u]);
+        }
+    }
 };
 
 // A range of a long row a workgroup.
@@ -659,7 +721,8 @@ __global__ __launch_bounds__(256) void k_logp_grad_rows(LogpGradArgs a, int chun
     const int chunk = (int)(blockIdx.x - row_in * chunks), tid = (int)threadIdx.x;
     const T* z = (const T*)a.z + r * a.C_buf;
     T* dz = (T*)a.dz + r * a.C_dbuf;
-    GradRow row(a, r, r, 0);
+    Alts<-1> none;
+    GradRow row(a, r, r, 0, none);
     if (row.far()) {
         __shared__ float s[3][4];
         Acc acc = nothing();
@@ -700,15 +763,15 @@ __global__ __launch_bounds__(256) void k_logp_grad_rows(LogpGradArgs a, int chun
     // the label's class and the alternatives again, once the rest is written
     __syncthreads();
     if (tid <= a.topk) {
-        const long long j = tid < a.topk ? a.top_index[r * a.topk + tid] : row.label;
+        const int j = tid < a.topk ? a.top_index[r * a.topk + tid] : row.label;
         // (the workgroup that wrote it: a vector belongs to the range it begins in)
-        const long long first = j < head || j >= tail ? j : head + (j - head) / V * V;
-        if (j >= 0 && j < a.C && first >= c0 && first < c1) dz[j] = from_f32<T>(row.at(a, to_f32(z[j]), (int)j, r, 0));
+        const int first = j < head || j >= tail ? j : head + (j - head) / V * V;
+        if (j >= 0 && j < a.C && first >= c0 && first < c1) dz[j] = from_f32<T>(row.at(a, to_f32(z[j]), j, r, 0));
     }
 }
 
 // Short rows, as k_logp_short: gradients go through LDS too, at `out`.
-template <typename T>
+template <typename T, int K>
 __global__ __launch_bounds__(256) void k_logp_grad_short(LogpGradArgs a, int out) {
     extern __shared__ __align__(16) char lds[];
     const int tid = (int)threadIdx.x, rows = (int)blockDim.x;
@@ -721,7 +784,8 @@ __global__ __launch_bounds__(256) void k_logp_grad_short(LogpGradArgs a, int out
         const int at = tid * ld * (int)sizeof(T), to = tid * a.C * (int)sizeof(T);
         auto get = [&](int c) { return to_f32(*(const T*)(lds + staged(at + c * (int)sizeof(T)))); };
         auto put = [&](int c, float v) { *(T*)(lds + out + staged(to + c * (int)sizeof(T))) = from_f32<T>(v); };
-        GradRow row(a, r, r, 0);
+        Alts<K> alts;
+        GradRow row(a, r, r, 0, alts);
         if (row.far()) {
             Acc acc = nothing();
             RegTop<0> none;
@@ -730,10 +794,13 @@ __global__ __launch_bounds__(256) void k_logp_grad_short(LogpGradArgs a, int out
         }
 #pragma unroll 4
         for (int c = 0; c < a.C; ++c) put(c, row.all(get(c)));
-        if (row.label >= 0 && row.label < a.C) put((int)row.label, row.at(a, get((int)row.label), (int)row.label, r, 0));
-        for (int i = 0; i < a.topk; ++i) {
-            const int j = a.top_index[r * a.topk + i];
-            if (j >= 0 && j < a.C) put(j, row.at(a, get(j), j, r, 0));
+        if (row.label >= 0) put(row.label, row.at(alts, get(row.label), row.label));
+        if constexpr (K > 0) {
+#pragma unroll
+            for (int u = 0; u < K; ++u)
+                if (alts.j[u] >= 0 && alts.j[u] < a.C) put(alts.j[u], row.at(alts, get(alts.j[u]), alts.j[u]));
+        } else if constexpr (K < 0) {
+            row.again(a, r, 0, 0, a.C, get, put);
         }
     }
     __syncthreads();
@@ -753,8 +820,11 @@ __global__ __launch_bounds__(256) void k_logp_grad_short(LogpGradArgs a, int out
     }
 }
 
-// Pixels of planes: a thread a pixel and range of classes.
-template <typename T>
+// Pixels of planes: a thread a pixel and range of classes.  The label and the
+// alternatives are looked for at every class, since a second write to a class here
+// and there costs more (4 x 256 x 512 pixels of 19 fp32 classes, no, one and three
+// alternatives: 24, 60 and 72 us, and so 15, 16 and 18).
+template <typename T, int K>
 __global__ __launch_bounds__(256) void k_logp_grad_planes(LogpGradArgs a, int per) {
     const long long r = (long long)blockIdx.x * 256 + threadIdx.x;
     if (r >= a.R) return;
@@ -763,7 +833,8 @@ __global__ __launch_bounds__(256) void k_logp_grad_planes(LogpGradArgs a, int pe
     T* dz = (T*)a.dz + n * a.C_dbuf * a.P + p;
     const int c0 = (int)blockIdx.y * per, c1 = min(a.C, c0 + per);
     auto get = [&](int c) { return to_f32(z[c * a.P]); };
-    GradRow row(a, r, n, p);
+    Alts<K> alts;
+    GradRow row(a, r, n, p, alts);
     if (row.far()) {
         Acc acc = nothing();
         RegTop<0> none;
@@ -771,12 +842,8 @@ __global__ __launch_bounds__(256) void k_logp_grad_planes(LogpGradArgs a, int pe
         row.take(acc);
     }
 #pragma unroll 8
-    for (int c = c0; c < c1; ++c) dz[c * a.P] = from_f32<T>(row.all(get(c)));
-    auto again = [&](long long j) {
-        if (j >= c0 && j < c1) dz[j * a.P] = from_f32<T>(row.at(a, get((int)j), (int)j, n, p));
-    };
-    again(row.label);
-    for (int i = 0; i < a.topk; ++i) again(a.top_index[(n * a.topk + i) * a.P + p]);
+    for (int c = c0; c < c1; ++c) dz[c * a.P] = from_f32<T>(row.at(alts, get(c), c));
+    if constexpr (K < 0) row.again(a, n, p, c0, c1, get, [&](int c, float v) { dz[c * a.P] = from_f32<T>(v); });
 }
 
 // ---------------------------------------------------------------------------
@@ -891,23 +958,32 @@ hipError_t logp_t(const LogpArgs& a, Ws ws, hipStream_t st) {
     return nw == 4 ? logp_rows<T, 4>(a, ws, st, 1) : logp_rows<T, 16>(a, ws, st, 1);
 }
 
-template <typename T>
-hipError_t grad_t(const LogpGradArgs& a, hipStream_t st) {
+template <typename T, int K>
+hipError_t grad_k(const LogpGradArgs& a, hipStream_t st, int rows) {
     if (is_planes(a.P)) {
         const long long wgs = (a.R + 255) / 256;
         // ranges of classes until there are eight workgroups a CU
         const int ranges = (int)std::max(1LL, std::min<long long>(2048 / wgs, a.C / 16));
         const int per = (a.C + ranges - 1) / ranges;
-        hipLaunchKernelGGL(k_logp_grad_planes<T>, dim3((unsigned)wgs, (a.C + per - 1) / per), dim3(256), 0, st, a, per);
-        return hipGetLastError();
-    }
-    if (const int rows = short_rows(sizeof(T), a.R, a.C, a.C_buf, true)) {
+        hipLaunchKernelGGL((k_logp_grad_planes<T, K>), dim3((unsigned)wgs, (a.C + per - 1) / per), dim3(256), 0, st, a, per);
+    } else {
         const int es = sizeof(T), out = (staged_bytes(((rows - 1) * (int)a.C_buf + a.C) * es + 16) + 15) / 16 * 16;
         const int lds = out + staged_bytes(rows * a.C * es + 16);
         if (lds > 64 * 1024)
-            if (hipError_t e = ensure_dyn_lds((const void*)k_logp_grad_short<T>, lds); e != hipSuccess) return e;
-        hipLaunchKernelGGL(k_logp_grad_short<T>, dim3((unsigned)((a.R + rows - 1) / rows)), dim3(rows), lds, st, a, out);
-        return hipGetLastError();
+            if (hipError_t e = ensure_dyn_lds((const void*)k_logp_grad_short<T, K>, lds); e != hipSuccess) return e;
+        hipLaunchKernelGGL((k_logp_grad_short<T, K>), dim3((unsigned)((a.R + rows - 1) / rows)), dim3(rows), lds, st, a, out);
+    }
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t grad_t(const LogpGradArgs& a, hipStream_t st) {
+    const int rows = is_planes(a.P) ? 0 : short_rows(sizeof(T), a.R, a.C, a.C_buf, true);
+    if (is_planes(a.P) || rows) {
+        if (a.topk > 8) return grad_k<T, -1>(a, st, rows);
+        if (a.topk == 0) return grad_k<T, 0>(a, st, rows);
+        if (a.topk == 1) return grad_k<T, 1>(a, st, rows);
+        return a.topk <= 4 ? grad_k<T, 4>(a, st, rows) : grad_k<T, 8>(a, st, rows);
     }
     // ranges of 4 vectors a thread, or 16 where rows are many
     const int per = 256 * LV<T> * (a.R * a.C >= (64LL << 20) ? 16 : 4);

@@ -14,7 +14,10 @@
 // the result (MAX_GROWTH) and the next one starts from a fresh X X^T: five
 // steps are blocks of 3 and 2 for fp32 and fp16, where the error is that of an
 // fp32 iteration (2.7e-6 of the norm against 2.1e-6 at 350 x 1500), and one
-// block for bf16 (2e-4, a tenth of its rounding).  All s x s matrices and all
+// block for bf16 (2e-4, a tenth of its rounding).  bf16 matrices that are not
+// long take single steps instead, a X + B X with B = b A + c A A, whose products
+// are of single fp16 numbers (2.1e-3 and not 1.7e-3 off, of which all but
+// 1.2e-3 is the result's rounding; go_direct).  Else all s x s matrices and all
 // X but the first are pairs of fp16 numbers hi + lo (22 bits and a sign) times
 // a power of two known beforehand from the polynomial's bounds; a product of
 // two is three MFMAs hi hi + hi lo + lo hi with fp32 sums.  The first X is one
@@ -1085,8 +1088,10 @@ struct Runner {
             a += n * steps * (3 * s * s * L + s * s * s);
             b += n * (5 * s * s * L + 3 * std::max(1, 4 * steps - 3) * s * s * s);
         }
-        // (MFMAs of both; single steps are a few launches more: bf16 512 x 1024 151 us and 162
-        // in blocks, 1024 x 1024 199 and 255, but 1024 x 4096 320 and 286)
+        // (MFMAs of both, where the blocks' are more of launches that do not fill the chip:
+        // single steps and blocks take for 1024 x 1024 184 and 254 us, at a = 0.57 b 4096 x 8192
+        // 3058 and 4146, at 0.92 b 512 x 2048 157 and 167, 2048 x 8192 988 and 983 and
+        // 4096 x 16384 5714 and 4857)
         return a < 0.75 * b;
     }
     hipError_t go_direct(int steps, const double* coef) {

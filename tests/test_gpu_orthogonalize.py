@@ -17,6 +17,10 @@ bound the worst spectrum.  The gradients here have directions between 1 and 1e-3
 of the largest with |A| below 0.3, errors of random sign and so a hundredth of
 that; what is asserted is a tenth, plus the rounding: fp32 2e-5, fp16 2^-11 + 2e-4,
 bf16 2^-8 + 2e-3.
+bf16 updates with sides not far apart take single steps a X + B X, whose factors
+are fp16: X and A once rounded in A and in B, B and X in B X, each of a norm of at
+most 2^-11 / sqrt(3) of its own and of random sign, so about 2 * 2^-11 / sqrt(3) =
+5.6e-4 a step of what a step adds, 1.3e-3 over five in squares, within the 2e-3.
 """
 from __future__ import annotations
 
