@@ -315,6 +315,28 @@ def test_grad_odd_rows(form):
     close(dz[keep], ref, 2.0 ** -16 * size + 2.0 ** -23 * ref.abs() + 1e-38, "dlogits")
 
 
+@pytest.mark.parametrize("topk", [3, 8, 12])
+@pytest.mark.parametrize("form", ["short", "rows", "planes"])
+def test_grad_of_a_class_named_twice(form, topk):
+    """Indices that name a class more than once, the label's among them: their gradients add up."""
+    log(f"[log_probs] gradient, a class named twice, {form}, top {topk}")
+    C, R = (21, 70) if form != "rows" else (3000, 5)
+    gen = torch.Generator().manual_seed(topk)
+    z, lab = torch.randn(R, C, generator=gen), torch.randint(0, C, (R,), generator=gen)
+    ti = torch.randint(0, 4, (R, topk), generator=gen).int()
+    ti[:, 1], ti[:, -1] = lab, lab
+    g, gt = torch.randn(R, generator=gen), torch.randn(R, topk, generator=gen)
+    ref, size = grad_reference(z.double(), lab, g.double(), None, ti.long(), gt.double())
+    up = (lambda x: x.reshape(1, R, 1, -1).permute(0, 3, 1, 2).contiguous().cuda()) if form == "planes" else (lambda x: x.cuda())
+    one = (lambda x: x.reshape(1, R, 1).cuda()) if form == "planes" else (lambda x: x.cuda())
+    lse = sb.log_probs(up(z))[1]
+    dz = sb.log_probs_backward(up(z), one(lab), lse, d_logp=one(g), top_index=up(ti), d_top=up(gt)).cpu()
+    dz = dz.movedim(1, -1).reshape(R, C) if form == "planes" else dz
+    # fp32: a sum of up to 14 terms, each sum rounded, beside what grad_reference's size allows for
+    many = gt.abs().sum(1, keepdim=True).double() + g.abs()[:, None]
+    close(dz, ref, 2.0 ** -16 * size + 14 * 2.0 ** -24 * many + 1e-38, "dlogits")
+
+
 def test_gradient_by_differences():
     gen = torch.Generator().manual_seed(8)
     z = torch.randn(6, 40, generator=gen).cuda()
