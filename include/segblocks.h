@@ -574,7 +574,9 @@ typedef struct {
  *   a matrix with more rows than columns is taken transposed),
  * written to out in `dtype`.  coefficients: HOST array of a, b, c for every
  * step (3 * steps).  1 <= steps <= 32, eps >= 0; a matrix of zeros gives
- * zeros, one with NaN or an infinity gives NaN.  The sums are fp32, and
+ * zeros, one with NaN or an infinity gives NaN.  A matrix has up to 2^34
+ * elements, a longer side of up to 2^23 and a shorter one of up to 32768.
+ * The sums are fp32, and
  * matrices between the products are held to 22 bits and a sign, so the result
  * is that of an fp32 iteration also for a 16-bit update, rounded once; but
  * for bf16 with up to five steps, where the sides are not far apart, factors

@@ -896,7 +896,9 @@ def _matrices(updates, outs=None):
 def orthogonalize_workspace_size(updates) -> int:
     """Bytes of workspace that orthogonalize needs for these updates (their
     shapes and type count)."""
-    updates = [updates] if isinstance(updates, torch.Tensor) else list(updates)
+    updates = [t for t in ([updates] if isinstance(updates, torch.Tensor) else updates) if t.numel()]
+    if not updates:
+        return 0
     n = ctypes.c_size_t(0)
     _b.call("segblocks_orthogonalize_workspace_size", _matrices(updates), len(updates), _dt(updates[0]), ctypes.byref(n))
     return int(n.value)

@@ -9,6 +9,7 @@
 #include <stdio.h>
 
 #include <algorithm>
+#include <functional>
 #include <mutex>
 #include <new>
 #include <string>
@@ -1185,7 +1186,8 @@ int check_matrices(const char* fn, const sb_matrix* mats, int count, int dtype, 
         if (q.batch <= 0 || q.rows <= 0 || q.cols <= 0)
             return fail(SB_EINVAL, fn, "batch, rows, cols of entry %d must be positive (got %d, %d, %d)", i, q.batch,
                         q.rows, q.cols);
-        if (std::min(q.rows, q.cols) > 32768 || std::max(q.rows, q.cols) > (1 << 26) ||
+        // (2^23: a tile's 128 rows of pairs are reached with 32-bit offsets)
+        if (std::min(q.rows, q.cols) > 32768 || std::max(q.rows, q.cols) > (1 << 23) ||
             (long long)q.rows * q.cols > (1LL << 34) || (long long)q.rows * q.cols * q.batch > (1LL << 36))
             return fail(SB_ESHAPE, fn, "entry %d is too large (%d x %d x %d)", i, q.batch, q.rows, q.cols);
         if (q.ld < q.cols || q.ld_out < q.cols)
@@ -1199,6 +1201,19 @@ int check_matrices(const char* fn, const sb_matrix* mats, int count, int dtype, 
                      q.batch > 1 ? q.batch_stride_out : 0, q.batch, q.rows, q.cols});
     }
     return SB_OK;
+}
+
+// any_overlap for long lists.
+bool list_overlap(std::vector<Range> outs, const std::vector<Range>& ins) {
+    auto before = [](const Range& a, const Range& b) { return std::less<const void*>()(a.p, b.p); };
+    std::sort(outs.begin(), outs.end(), before);
+    for (size_t i = 1; i < outs.size(); ++i)
+        if (overlap(outs[i - 1], outs[i])) return true;
+    for (const Range& r : ins) {
+        const auto at = std::upper_bound(outs.begin(), outs.end(), r, before);
+        if ((at != outs.end() && overlap(*at, r)) || (at != outs.begin() && overlap(*(at - 1), r))) return true;
+    }
+    return false;
 }
 
 }  // namespace
@@ -1225,7 +1240,7 @@ int segblocks_orthogonalize(const sb_matrix* matrices, int count, int dtype, int
     const size_t need = sb::orth_ws_bytes(dtype, v.data(), count);
     if ((s = check_ws(fn, need, workspace, ws_bytes))) return s;
     outs.push_back({workspace, (long long)need});
-    if (any_overlap(outs, ins)) return fail(SB_EINVAL, fn, "outputs or the workspace overlap inputs or each other");
+    if (list_overlap(outs, ins)) return fail(SB_EINVAL, fn, "outputs or the workspace overlap inputs or each other");
     return hip_status(fn, sb::launch_orth(dtype, v.data(), count, steps, coefficients, eps, sb::Ws{workspace, need},
                                           stream));
 } catch (const std::bad_alloc&) {  // (the lists above, on the host)

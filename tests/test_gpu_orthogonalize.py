@@ -243,6 +243,28 @@ def test_single_rows_columns_and_wide_slices(dtype):
         near(o, reference(g), TOL[dtype], f"{tuple(g.shape)} of strides {g.stride()}")
 
 
+@pytest.mark.parametrize("tall", [False, True])
+def test_the_longest_side(tall):
+    """Rows whose offsets in the workspace pass 2^31 (63 rows of 2^23 pairs), the last columns among them."""
+    if torch.cuda.mem_get_info()[0] < 60 << 30:
+        pytest.skip("needs 60 GB of free memory")
+    log(f"[orthogonalize] the longest side, tall {tall}")
+    torch.manual_seed(3)
+    g = torch.randn(60, 1 << 23, dtype=torch.bfloat16, device="cuda")
+    o = sb.orthogonalize(g.t().contiguous()).t() if tall else sb.orthogonalize(g)
+    x = g.double()
+    f = 1 / (x.norm().item() + 1e-7)
+    A = (x @ x.t()).cpu() * f * f
+    (a, b, c), Q, one = ABC, torch.eye(60, dtype=torch.float64), torch.eye(60, dtype=torch.float64)
+    for _ in range(5):
+        P = a * one + b * A + c * (A @ A)
+        Q, A = P @ Q, P @ A @ P
+    ref = (Q * f).cuda() @ x
+    for part in (slice(None), slice(-64, None)):  # (the rows are nearly orthogonal: all parts are off alike)
+        off = ((o[:, part].double() - ref[:, part]).norm() / ref[:, part].norm()).item()
+        assert off <= TOL["bf16"], f"{off:.2e} off"
+
+
 def test_empty_updates_and_lists():
     assert sb.orthogonalize([]) == []
     assert sb.orthogonalize(torch.empty(0, 5, device="cuda")).shape == (0, 5)

@@ -93,7 +93,46 @@ def test_orthogonalize_refuses(lib, kw, code, msg):
     assert msg in lib.segblocks_last_error().decode()
 
 
+def test_sides_with_32_bit_offsets_are_taken_and_longer_ones_refused(lib):
+    # 127 rows of L pairs of 4 bytes, and a row's 128 bytes, lie below 2^32
+    assert 127 * 4 * (1 << 23) + 128 < 1 << 32
+    n = ctypes.c_size_t(0)
+    for cols, code in ((1 << 23, 0), ((1 << 23) + 1, -2)):
+        for swap in (False, True):
+            m, k = (cols, 64) if swap else (64, cols)
+            q = b.Matrix(batch=1, rows=m, cols=k, ld=k, ld_out=k)
+            assert lib.segblocks_orthogonalize_workspace_size(ctypes.pointer(q), 1, 2, ctypes.byref(n)) == code
+    assert "too large" in lib.segblocks_last_error().decode()
+
+
+def test_a_long_list_finds_its_overlaps(lib):
+    """4096 outputs in any order; one that reaches into the next, and an update inside an output."""
+    def call(change):
+        mats = (b.Matrix * 4096)()
+        for i, q in enumerate(mats):
+            j = i * 1237 % 4096  # (odd: every place once)
+            q.batch, q.rows, q.cols, q.ld, q.ld_out = 1, 4, 16, 16, 16
+            q.update, q.out = 0x100000000 + j * 128, 0x200000000 + j * 128
+        change(mats)
+        c = (ctypes.c_double * 3)(1.0, 0.0, 0.0)
+        n = ctypes.c_size_t(0)
+        assert lib.segblocks_orthogonalize_workspace_size(mats, 4096, 2, ctypes.byref(n)) == 0
+        return lib.segblocks_orthogonalize(mats, 4096, 2, 1, c, 0.0, ctypes.c_void_p(0x900000000), n.value, None)
+
+    def grow(mats):
+        mats[2000].rows = 5
+
+    def inside(mats):
+        mats[7].update = mats[3000].out + 64
+
+    for change in (grow, inside):
+        assert call(change) == -1
+        assert "overlap" in lib.segblocks_last_error().decode()
+
+
 def test_workspace_queries():
+    assert sb.orthogonalize_workspace_size([]) == 0
+    assert sb.orthogonalize_workspace_size([torch.empty(0, 3), torch.empty(4, 4)]) == sb.orthogonalize_workspace_size(torch.empty(4, 4))
     bf = torch.bfloat16
     assert sb.log_probs_workspace_size(bf, b.SB_NHWC, 4096, 50000, 1, 1, 50000, 5) == 0
     assert sb.log_probs_workspace_size(bf, b.SB_NHWC, 1, 131072, 1, 1, 131072, 5) > 0
