@@ -347,6 +347,8 @@ __device__ __forceinline__ void dma16(const char* from, unsigned char* to) {
 // 100 us, MFMAs with their LDS reads alone 112, together 207 and spread 196 (1.08
 // PFLOP/s of MFMA, where a large library product reaches 1.21).  More stages (one
 // workgroup of eight waves a CU), or operands read a stage ahead, were no faster.
+// Of single numbers it takes 84 us (0.82 PFLOP/s, DMA and MFMAs in turn), and in steps
+// of 32, whose instructions touch twice the lines for half of each, 106.
 template <int T, int NA, int NB, int SA, int SB>
 __device__ __forceinline__ void product_tile(const char* A, long long pa, const char* B, long long pb, int step0,
                                              int steps, unsigned char* lds) {
@@ -645,7 +647,8 @@ __global__ __launch_bounds__(NT<T>) void k_orth_join(Table tb, SymLaunch s) {
 // A block of steps on matrices of one tile (s <= 64) without leaving a workgroup:
 // from the sums of X X^T to Q, everything in LDS.  As launches of their own its
 // products took 4.6 us each, whatever they compute (a filter of 64 x 576, 13
-// products: 60 us; here the whole block takes 7.4 to 11 us).  Four waves a product, the eight share T and Q.
+// products: 60 us; here the whole block takes 7.4 to 11 us).  Four waves a product,
+// the eight share T and Q.
 struct Steps {
     int len, first, Q;  // Q: where it goes
     float a0, eps;      // A = a0 f^2 X X^T
