@@ -576,12 +576,8 @@ typedef struct {
  * step (3 * steps).  1 <= steps <= 32, eps >= 0; a matrix of zeros gives
  * zeros, one with NaN or an infinity gives NaN.  A matrix has up to 2^34
  * elements, a longer side of up to 2^23 and a shorter one of up to 32768.
- * The sums are fp32, and
- * matrices between the products are held to 22 bits and a sign, so the result
- * is that of an fp32 iteration also for a 16-bit update, rounded once; but
- * for bf16 with up to five steps, where the sides are not far apart, factors
- * of products are rounded to 11 bits (fp16), which adds about 1.2e-3 of the
- * norm to the 1.7e-3 of the result's own rounding.  Workspace:
+ * The sums are fp32, and matrices between the products are held to 22 bits
+ * and a sign, for 16-bit updates too, whose result is rounded once.  Workspace:
  * segblocks_orthogonalize_workspace_size (a function of the entries' sizes,
  * pointers not looked at). */
 int segblocks_orthogonalize(const sb_matrix* matrices, int count, int dtype, int steps, const double* coefficients,

@@ -14,15 +14,16 @@
 // the result (MAX_GROWTH) and the next one starts from a fresh X X^T: five
 // steps are blocks of 3 and 2 for fp32 and fp16, where the error is that of an
 // fp32 iteration (2.7e-6 of the norm against 2.1e-6 at 350 x 1500), and one
-// block for bf16 (2e-4, a tenth of its rounding).  bf16 matrices that are not
-// long take single steps instead, a X + B X with B = b A + c A A, whose products
-// are of single fp16 numbers (2.1e-3 and not 1.7e-3 off, of which all but
-// 1.2e-3 is the result's rounding; go_direct).  Else all s x s matrices and all
+// block for bf16 (2e-4, a tenth of its rounding).  All s x s matrices and all
 // X but the first are pairs of fp16 numbers hi + lo (22 bits and a sign) times
 // a power of two known beforehand from the polynomial's bounds; a product of
-// two is three MFMAs hi hi + hi lo + lo hi with fp32 sums.  The first X is one
-// fp16 number for 16-bit updates (fp16 as it is, bf16 times a power of two:
-// values below 2^-38 of the largest are cut) and a pair for fp32.
+// two is three MFMAs hi hi + hi lo + lo hi with fp32 sums.  (Single fp16 numbers
+// are too few for 16-bit updates too: the slopes of later steps multiply their
+// rounding, which adds 1e-3 to 2e-3 of the norm for spectra without large
+// gaps, 8e-3 for four directions alike, and 0.1 with coefficients that are
+// steeper.)  The first X is one fp16 number for 16-bit updates (fp16 as it is,
+// bf16 times a power of two: values below 2^-38 of the largest are cut) and a
+// pair for fp32.
 #include <math.h>
 
 #include <algorithm>
@@ -105,17 +106,16 @@ __host__ __device__ inline int prep_wgs(const OMat& q) {
 
 // ---------------------------------------------------------------------------
 // Storage of a matrix (S), rows of one of
-//   ONES     [k], single numbers
-//   PAIRS    [k / 32][32 hi | 32 lo], for products that take both
-//   HI_PAIRS [k / 64][64 hi | 64 lo], for products that take hi alone
-// so that a product's step reads whole lines of 128 bytes.
+//   ONES   [k], single numbers
+//   PAIRS  [k / 32][32 hi | 32 lo]
+// so that a product's step reads whole lines of 128 bytes.  The value is the count
+// of numbers of an element.
 // ---------------------------------------------------------------------------
-enum { ONES = 1, PAIRS = 2, HI_PAIRS = 3 };
-template <int S> constexpr int BYTES = S == ONES ? 2 : 4;           // of an element
-template <int S> constexpr int LO_AT = S == HI_PAIRS ? 128 : 64;    // from hi to lo
+enum { ONES = 1, PAIRS = 2 };
+constexpr int LO_AT = 64;  // bytes from hi to lo
 template <int S>
 __device__ __forceinline__ long long at_k(long long k) {  // bytes, k a multiple of 8
-    return S == ONES ? k * 2 : S == PAIRS ? (k >> 5) * 128 + (k & 31) * 2 : (k >> 6) * 256 + (k & 63) * 2;
+    return S == ONES ? k * 2 : (k >> 5) * 128 + (k & 31) * 2;
 }
 
 template <int S>
@@ -134,7 +134,7 @@ __device__ __forceinline__ void store8(char* row, long long k, const float (&v)[
     }
     char* p = row + at_k<S>(k);
     vstore<f16, 8>((f16*)p, hi);
-    if (S != ONES) vstore<f16, 8>((f16*)(p + LO_AT<S>), lo);
+    if (S == PAIRS) vstore<f16, 8>((f16*)(p + LO_AT), lo);
 }
 
 // An R x T piece in LDS (fp32, rows CP<T> apart) to rows r0.. and columns c0.. of a
@@ -154,7 +154,7 @@ __device__ __forceinline__ void store_tile(const float* C, char* dst, long long 
         float v[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = TURNED ? C[(k + i) * CP<T> + r] : C[r * CP<T> + k + i];
-        store8<S>(dst + (long long)(r0 + r) * K * BYTES<S>, c0 + k, v);
+        store8<S>(dst + (long long)(r0 + r) * K * (2 * S), c0 + k, v);
     }
 }
 
@@ -339,7 +339,7 @@ __device__ __forceinline__ void dma16(const char* from, unsigned char* to) {
 }
 
 // rows of A and B from their first element on; the tile ends in LDS as fp32.  NA,
-// NB: numbers of an element that take part, SA, SB: how they are stored.
+// NB: how they are stored.
 //
 // A wave's DMA instructions are spread over its MFMAs: a CU takes one (1 KB) in
 // about 28 cycles, and a wave that issues a stage's eight in a row stands still
@@ -349,11 +349,10 @@ __device__ __forceinline__ void dma16(const char* from, unsigned char* to) {
 // workgroup of eight waves a CU), or operands read a stage ahead, were no faster.
 // Of single numbers it takes 84 us (0.82 PFLOP/s, DMA and MFMAs in turn), and in steps
 // of 32, whose instructions touch twice the lines for half of each, 106.
-template <int T, int NA, int NB, int SA, int SB>
+template <int T, int NA, int NB>
 __device__ __forceinline__ void product_tile(const char* A, long long pa, const char* B, long long pb, int step0,
                                              int steps, unsigned char* lds) {
     constexpr bool ONE = NA + NB == 2;
-    static_assert(ONE || (SA == NA && SB == NB), "steps of 32 of what is stored");
     constexpr int RA = ONE ? 128 : 64 * NA, RB = ONE ? 128 : 64 * NB;  // bytes of a row and step
     constexpr int STAGE = stage_bytes<T, NA, NB>(), OB = T * RA, STEP = T * (RA + RB), NST = stages<T, NA, NB>();
     // Two groups of four waves take steps of 32 in turn, or halves of one step of 64.
@@ -362,8 +361,6 @@ __device__ __forceinline__ void product_tile(const char* A, long long pa, const 
     constexpr int LA = T * RA / 16 / LOADERS, LB = T * RB / 16 / LOADERS, LH = LA + LB;
     constexpr int LOADS = ONE ? LH : STEPS * LH / GROUPS;
     static_assert(ONE || STEPS % GROUPS == 0, "a group takes whole steps of 32");
-    // bytes that a step takes along a stored row
-    constexpr long long GA = ONE ? 64 * BYTES<SA> : RA, GB = ONE ? 64 * BYTES<SB> : RB;
     // the three products of a 64 x 64 tile's one fragment in sums of their own:
     // an MFMA waits for the one before it on the same sum
     constexpr int CH = T == 64 ? NA + NB - 1 : 1;
@@ -382,7 +379,7 @@ __device__ __forceinline__ void product_tile(const char* A, long long pa, const 
     }
     auto dma = [&](int i, int s, int buf) {  // instruction i of stage s
         const int k = ONE ? 0 : i / LH * GROUPS + group, j = i % LH;
-        const char* base = (j < LA ? A : B) + ((long long)(step0 + s) * STEPS + k) * (j < LA ? GA : GB);
+        const char* base = (j < LA ? A : B) + ((long long)(step0 + s) * STEPS + k) * (j < LA ? RA : RB);
         unsigned char* to = lds + buf * STAGE + k * STEP + (j < LA ? j : j - LA) * (LOADERS * 16) + (j < LA ? 0 : OB) +
                             loader * 1024;
         dma16(base + from[j], to);
@@ -492,30 +489,29 @@ __device__ __forceinline__ void sym_tile(int t, int n, int& bi, int& bj) {
 
 // out = alpha C + beta D + gamma I for R x T cells at (r0, c0) of symmetric
 // matrices [sp][sp], and their mirror image.
-template <int T, int R, int S>
+template <int T, int R>
 __device__ __forceinline__ void store_sym(float* C, char* out, const char* D, int sp, int r0, int c0, bool mirror,
                                           float alpha, float beta, float gamma) {
     for (int e = (int)threadIdx.x; e < R * T / 8; e += NT<T>) {
         const int r = e / (T / 8), k = (e % (T / 8)) * 8, K = c0 + k;
-        const long long row = (long long)(r0 + r) * sp * BYTES<S>;
+        const long long row = (long long)(r0 + r) * sp * 4;
         float v[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = alpha * C[r * CP<T> + k + i];
         if (D) {
-            const Vec<f16, 8> hi = vload<f16, 8>((const f16*)(D + row + at_k<S>(K)));
-            Vec<f16, 8> lo = vzero<f16, 8>();
-            if (S != ONES) lo = vload<f16, 8>((const f16*)(D + row + at_k<S>(K) + LO_AT<S>));
+            const Vec<f16, 8> hi = vload<f16, 8>((const f16*)(D + row + at_k<PAIRS>(K)));
+            const Vec<f16, 8> lo = vload<f16, 8>((const f16*)(D + row + at_k<PAIRS>(K) + LO_AT));
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 v[i] += beta * ((float)hi.e[i] + (float)lo.e[i]) + (r0 + r == K + i ? gamma : 0.0f);
         }
-        store8<S>(out + row, K, v);
+        store8<PAIRS>(out + row, K, v);
 #pragma unroll
         for (int i = 0; i < 8; ++i) C[r * CP<T> + k + i] = v[i];
     }
     if (!mirror) return;
     __syncthreads();
-    store_tile<T, S, true, R>(C, out, sp, c0, r0);
+    store_tile<T, PAIRS, true, R>(C, out, sp, c0, r0);
 }
 
 // One or two products that give symmetric matrices (numbers of the
@@ -559,7 +555,7 @@ __device__ __forceinline__ SymUnit sym_unit(const Table& tb, const SymLaunch& s,
 }
 
 // C: R rows of the tile from row `part` R on.
-template <int T, int R, int O, bool GRAM>
+template <int T, int R, bool GRAM>
 __device__ __forceinline__ void sym_out(const OMat& q, char* ws, const SymLaunch& s, const SymJob& j, int t, int part,
                                         float* C) {
     int bi, bj;
@@ -570,11 +566,11 @@ __device__ __forceinline__ void sym_out(const OMat& q, char* ws, const SymLaunch
         const float f = norm_factor(q, ws, s.eps);
         alpha *= f * f;
     }
-    store_sym<T, R, O>(C, sym(j.c), GRAM || j.d < 0 ? nullptr : sym(j.d), q.sp, bi * T + part * R, bj * T, bi != bj,
-                       alpha, j.beta, j.gamma);
+    store_sym<T, R>(C, sym(j.c), GRAM || j.d < 0 ? nullptr : sym(j.d), q.sp, bi * T + part * R, bj * T, bi != bj,
+                    alpha, j.beta, j.gamma);
 }
 
-template <int T, int NP, int S, int O, bool GRAM>  // NP numbers of what is stored as S take part; O: how the result is
+template <int T, int S, bool GRAM>
 __global__ __launch_bounds__(NT<T>, 2) void k_orth_sym(Table tb, SymLaunch s) {
     extern __shared__ __align__(16) unsigned char lds[];
     const SymUnit u = sym_unit<T>(tb, s, (int)blockIdx.x);
@@ -583,12 +579,12 @@ __global__ __launch_bounds__(NT<T>, 2) void k_orth_sym(Table tb, SymLaunch s) {
     char* ws = q.ws + u.p.b * q.ws_one;
     int bi, bj;
     sym_tile(u.p.t, q.sp / T, bi, bj);
-    const int K = GRAM ? q.Lp : q.sp, steps = K / STEP_K<T, NP, NP>;
+    const int K = GRAM ? q.Lp : q.sp, steps = K / STEP_K<T, S, S>;
     const int k0 = (int)((long long)steps * u.part / u.parts), k1 = (int)((long long)steps * (u.part + 1) / u.parts);
-    const long long pitch = (long long)K * BYTES<S>;
+    const long long pitch = (long long)K * (2 * S);
     const char* A = GRAM ? ws + w_x(q.sp, q.Lp, s.x) : ws + w_sym(q.sp, q.Lp, j.a);
     const char* B = GRAM ? A : ws + w_sym(q.sp, q.Lp, j.b);
-    product_tile<T, NP, NP, S, S>(A + bi * T * pitch, pitch, B + bj * T * pitch, pitch, k0, k1 - k0, lds);
+    product_tile<T, S, S>(A + bi * T * pitch, pitch, B + bj * T * pitch, pitch, k0, k1 - k0, lds);
     float* C = (float*)lds;
     if (u.parts > 1 || s.leave) {
         float4* out = (float4*)(s.sums + u.unit * (T * T));
@@ -598,12 +594,12 @@ __global__ __launch_bounds__(NT<T>, 2) void k_orth_sym(Table tb, SymLaunch s) {
         }
         return;
     }
-    sym_out<T, T, O, GRAM>(q, ws, s, j, u.p.t, 0, C);
+    sym_out<T, T, GRAM>(q, ws, s, j, u.p.t, 0, C);
 }
 
 // The parts of the split tiles added in their order, a few rows a workgroup.
 template <int T> constexpr int JOIN_ROWS = T == 64 ? 32 : 16;
-template <int T, int O, bool GRAM>
+template <int T, bool GRAM>
 __global__ __launch_bounds__(NT<T>) void k_orth_join(Table tb, SymLaunch s) {
     constexpr int R = JOIN_ROWS<T>, N = R * T / 4 / NT<T>;  // vectors of a thread
     __shared__ float C[R * CP<T>];
@@ -641,7 +637,7 @@ __global__ __launch_bounds__(NT<T>) void k_orth_join(Table tb, SymLaunch s) {
         c[3] = sum[i].w;
     }
     __syncthreads();
-    sym_out<T, R, O, GRAM>(q, q.ws + u.p.b * q.ws_one, s, s.job[u.job], u.p.t, slice, C);
+    sym_out<T, R, GRAM>(q, q.ws + u.p.b * q.ws_one, s, s.job[u.job], u.p.t, slice, C);
 }
 
 // A block of steps on matrices of one tile (s <= 64) without leaving a workgroup:
@@ -770,56 +766,35 @@ __global__ __launch_bounds__(512) void k_orth_steps(Table tb, Steps st) {
     }
 }
 
-// Q X: the next block's X and its transpose, or the result.  DIRECT: the single
-// step a X + B X instead, Q being B, where both factors of the product are their
-// hi alone (B is stored as that) and a X has what X has.  S: how X is stored.
+// Q X: the next block's X and its transpose, or the result.  S: how X is stored.
 struct Apply {
     int Q, xt, first;
-    float alpha, a, eps;  // alpha Q X + a X
+    float alpha, eps;
 };
-template <int T, int S, typename TO, bool LAST, bool DIRECT>
+template <int T, int S, typename TO, bool LAST>
 __global__ __launch_bounds__(NT<T>, 2) void k_orth_apply(Table tb, Apply ap) {
     extern __shared__ __align__(16) unsigned char lds[];
-    constexpr int NQ = DIRECT ? 1 : 2, NX = DIRECT ? 1 : S, SQ = DIRECT ? ONES : PAIRS;
     const Place p = place(tb, [](const OMat& q) { return (q.sp / T) * (q.Lp / T); }, (int)blockIdx.x);
     const OMat& q = tb.mat[p.mat];
     char* ws = q.ws + p.b * q.ws_one;
     // strips of eight rows of Q, each along L
     const int strip = p.t / (8 * (q.Lp / T)), h = min(8, q.sp / T - 8 * strip), local = p.t - strip * (8 * (q.Lp / T));
     const int k = local / h, i = 8 * strip + (local - k * h);
-    const long long pq = (long long)q.sp * BYTES<SQ>, px = (long long)q.sp * BYTES<S>;
-    const char* X = ws + w_x(q.sp, q.Lp, ap.xt);
-    const char* Xt = ws + w_xt(q.sp, q.Lp, ap.xt);
+    const long long pq = (long long)q.sp * 4, px = (long long)q.sp * (2 * S);
     const char* qm = ws + w_sym(q.sp, q.Lp, ap.Q) + i * T * pq;
-    const char* xm = Xt + k * T * px;
-    const bool tall = LAST && q.m > q.n;  // then the tile's rows are those of Xt
-    const int steps = q.sp / STEP_K<T, NQ, NX>;
-    if (tall) product_tile<T, NX, NQ, S, SQ>(xm, px, qm, pq, 0, steps, lds);
-    else product_tile<T, NQ, NX, SQ, S>(qm, pq, xm, px, 0, steps, lds);
+    const char* xm = ws + w_xt(q.sp, q.Lp, ap.xt) + k * T * px;
+    const bool tall = LAST && q.m > q.n;  // then the tile's rows are those of the transpose
+    const int steps = q.sp / STEP_K<T, PAIRS, S>;
+    if (tall) product_tile<T, S, PAIRS>(xm, px, qm, pq, 0, steps, lds);
+    else product_tile<T, PAIRS, S>(qm, pq, xm, px, 0, steps, lds);
     float* C = (float*)lds;
-    const float f = ap.first ? norm_factor(q, ws, ap.eps) : 1.0f;
-    {  // each thread its own eights
-        const float alpha = f * ap.alpha, a = f * ap.a;
-        const char* D = tall ? Xt : X;
-        const int r0 = (tall ? k : i) * T, c0 = (tall ? i : k) * T;
-        const long long pd = (long long)(tall ? q.sp : q.Lp) * BYTES<S>;
-        for (int e = (int)threadIdx.x; e < T * T / 8; e += NT<T>) {
-            const int r = e / (T / 8), c = (e % (T / 8)) * 8;
-            float* v = C + r * CP<T> + c;
-            if constexpr (DIRECT) {
-                const char* d = D + (r0 + r) * pd + at_k<S>(c0 + c);
-                const Vec<f16, 8> hi = vload<f16, 8>((const f16*)d);
-                Vec<f16, 8> lo = vzero<f16, 8>();
-                if (S != ONES) lo = vload<f16, 8>((const f16*)(d + LO_AT<S>));
+    const float alpha = (ap.first ? norm_factor(q, ws, ap.eps) : 1.0f) * ap.alpha;
+    for (int e = (int)threadIdx.x; e < T * T / 8; e += NT<T>) {  // each thread its own eights
+        float* v = C + e / (T / 8) * CP<T> + e % (T / 8) * 8;
 #pragma unroll
-                for (int x = 0; x < 8; ++x) v[x] = alpha * v[x] + a * ((float)hi.e[x] + (float)lo.e[x]);
-            } else {
-#pragma unroll
-                for (int x = 0; x < 8; ++x) v[x] *= alpha;
-            }
-        }
-        __syncthreads();
+        for (int x = 0; x < 8; ++x) v[x] *= alpha;
     }
+    __syncthreads();
     if constexpr (LAST) {
         TO* o = (TO*)q.o + p.b * q.bstride_o;
         const int r0 = (tall ? k : i) * T, c0 = (tall ? i : k) * T;
@@ -837,9 +812,8 @@ __global__ __launch_bounds__(NT<T>, 2) void k_orth_apply(Table tb, Apply ap) {
                     if (c + n < q.n) to[n] = v.e[n];
         }
     } else {
-        constexpr int O = DIRECT ? HI_PAIRS : PAIRS;
-        store_tile<T, O, false>(C, ws + w_x(q.sp, q.Lp, ap.xt ^ 1), q.Lp, i * T, k * T);
-        store_tile<T, O, true>(C, ws + w_xt(q.sp, q.Lp, ap.xt ^ 1), q.sp, k * T, i * T);
+        store_tile<T, PAIRS, false>(C, ws + w_x(q.sp, q.Lp, ap.xt ^ 1), q.Lp, i * T, k * T);
+        store_tile<T, PAIRS, true>(C, ws + w_xt(q.sp, q.Lp, ap.xt ^ 1), q.sp, k * T, i * T);
     }
 }
 
@@ -1000,7 +974,7 @@ float pow2(int e) { return (float)ldexp(1.0, std::max(-140, std::min(120, e))); 
 
 template <typename T>
 struct Runner {
-    static constexpr int NP = sizeof(T) == 4 ? 2 : 1;  // numbers of an element of the first X, and its storage
+    static constexpr int FIRST = sizeof(T) == 4 ? PAIRS : ONES;  // how the first X is stored
     // (see the head of this file)
     static constexpr double MAX_GROWTH = std::is_same<T, bf16>::value ? 2.1e4 : std::is_same<T, f16>::value ? 150.0 : 12.5;
     Table& tb;
@@ -1029,9 +1003,9 @@ struct Runner {
         err = hipGetLastError();
     }
 
-    template <int TILE, int P, int S, int O, bool GRAM>
+    template <int TILE, int S, bool GRAM>
     void sym_t(SymLaunch& s, int jobs) {
-        constexpr int lds = product_lds<TILE, P, P>(), SLICES = TILE / JOIN_ROWS<TILE>;
+        constexpr int lds = product_lds<TILE, S, S>(), SLICES = TILE / JOIN_ROWS<TILE>;
         auto tiles = [](const OMat& q) { const int t = q.sp / TILE; return t * (t + 1) / 2; };
         s.sums = sums;
         s.eps = eps;
@@ -1039,9 +1013,9 @@ struct Runner {
         if (GRAM && (s.tiles < SLOTS || s.leave)) {
             gram_units(tb, TILE);
             s.whole = -1;
-            run<NT<TILE>>(k_orth_sym<TILE, P, S, O, GRAM>, number(tb, [&](const OMat& q) { return tiles(q) * q.parts; }), lds, s);
+            run<NT<TILE>>(k_orth_sym<TILE, S, GRAM>, number(tb, [&](const OMat& q) { return tiles(q) * q.parts; }), lds, s);
             if (!s.leave)
-                run<NT<TILE>>(k_orth_join<TILE, O, GRAM>,
+                run<NT<TILE>>(k_orth_join<TILE, GRAM>,
                               number(tb, [&](const OMat& q) { return q.parts > 1 ? tiles(q) * SLICES : 0; }), 0, s);
             return;
         }
@@ -1049,84 +1023,38 @@ struct Runner {
         s.whole = c.whole;
         s.parts = c.parts;
         const int rest = s.tiles * jobs - c.whole;
-        run<NT<TILE>>(k_orth_sym<TILE, P, S, O, GRAM>, (unsigned)(c.whole + rest * c.parts), lds, s);
-        if (rest) run<NT<TILE>>(k_orth_join<TILE, O, GRAM>, (unsigned)(rest * SLICES), 0, s);
+        run<NT<TILE>>(k_orth_sym<TILE, S, GRAM>, (unsigned)(c.whole + rest * c.parts), lds, s);
+        if (rest) run<NT<TILE>>(k_orth_join<TILE, GRAM>, (unsigned)(rest * SLICES), 0, s);
     }
-    template <int P, int S, int O, bool GRAM>
+    template <int S, bool GRAM>
     void sym(SymLaunch s, int jobs = 1) {
-        if (tile_of(sym_count(tb, 128) * jobs, wide) == 128) sym_t<128, P, S, O, GRAM>(s, jobs);
-        else sym_t<64, P, S, O, GRAM>(s, jobs);
+        if (tile_of(sym_count(tb, 128) * jobs, wide) == 128) sym_t<128, S, GRAM>(s, jobs);
+        else sym_t<64, S, GRAM>(s, jobs);
     }
-    void products(const SymJob& a) { sym<2, PAIRS, PAIRS, false>(SymLaunch{{a, a}}); }
-    void products(const SymJob& a, const SymJob& b) { sym<2, PAIRS, PAIRS, false>(SymLaunch{{a, b}}, 2); }
+    void products(const SymJob& a) { sym<PAIRS, false>(SymLaunch{{a, a}}); }
+    void products(const SymJob& a, const SymJob& b) { sym<PAIRS, false>(SymLaunch{{a, b}}, 2); }
 
-    template <int TILE, int S, bool LAST, bool DIRECT>
+    template <int TILE, int S, bool LAST>
     void apply_t(const Apply& ap) {
-        run<NT<TILE>>(k_orth_apply<TILE, S, T, LAST, DIRECT>,
+        run<NT<TILE>>(k_orth_apply<TILE, S, T, LAST>,
                       number(tb, [](const OMat& q) { return (q.sp / TILE) * (q.Lp / TILE); }),
-                      product_lds<TILE, DIRECT ? 1 : 2, DIRECT ? 1 : S>(), ap);
+                      product_lds<TILE, PAIRS, S>(), ap);
     }
-    template <int S, bool LAST, bool DIRECT>
+    template <int S, bool LAST>
     void apply(const Apply& ap) {
         long long n = 0;
         for (int i = 0; i < tb.count; ++i) n += (long long)(tb.mat[i].sp / 128) * (tb.mat[i].Lp / 128) * tb.mat[i].batch;
-        if (tile_of(n, wide) == 128) apply_t<128, S, LAST, DIRECT>(ap);
-        else apply_t<64, S, LAST, DIRECT>(ap);
+        if (tile_of(n, wide) == 128) apply_t<128, S, LAST>(ap);
+        else apply_t<64, S, LAST>(ap);
     }
-    template <bool DIRECT>
     void apply(const Apply& ap, bool last) {
-        constexpr int S = DIRECT ? HI_PAIRS : PAIRS;  // (of X after the first)
-        if (ap.first) last ? apply<NP, true, DIRECT>(ap) : apply<NP, false, DIRECT>(ap);
-        else last ? apply<S, true, DIRECT>(ap) : apply<S, false, DIRECT>(ap);
-    }
-
-    // One step at a time with products of single fp16 numbers, for bf16 alone (the
-    // head of this file): where it takes fewer of them than blocks do.
-    bool direct(int steps) const {
-        // (past five steps the slopes of the polynomial near 1 add up these roundings: 2.4e-3 at six)
-        if (!std::is_same<T, bf16>::value || single || steps > 5) return false;
-        double a = 0, b = 0;
-        for (int i = 0; i < tb.count; ++i) {
-            const double s = tb.mat[i].sp, L = tb.mat[i].Lp, n = tb.mat[i].batch;
-            a += n * steps * (3 * s * s * L + s * s * s);
-            b += n * (5 * s * s * L + 3 * std::max(1, 4 * steps - 3) * s * s * s);
-        }
-        // (MFMAs of both, where the blocks' are more of launches that do not fill the chip:
-        // single steps and blocks take for 1024 x 1024 184 and 254 us, at a = 0.57 b 4096 x 8192
-        // 3058 and 4146, at 0.92 b 512 x 2048 157 and 167, 2048 x 8192 988 and 983 and
-        // 4096 x 16384 5714 and 4857)
-        return a < 0.75 * b;
-    }
-    hipError_t go_direct(int steps, const double* coef) {
-        double lambda = 1.0;
-        int ex = 0;
-        for (int k = 0; k < steps; ++k) {
-            const double* c = coef + 3 * k;
-            const Bound b = bound_of(c, lambda);
-            const bool last = k + 1 == steps;
-            auto q = [&](double y) { return y > 0.0 && y <= lambda ? fabs(y * (c[1] + y * c[2])) : 0.0; };
-            const double bb = std::max(q(lambda), c[2] != 0.0 ? q(-c[1] / (2.0 * c[2])) : 0.0);
-            const int ea = exponent(lambda), eb = exponent(std::min(std::max(bb, 1e-30), 1e30));
-            const int ex2 = last ? 0 : exponent(sqrt(b.lambda));
-            SymLaunch s{{{0, 0, 0, -1, pow2(ea - 2 * ex), 0.0f, 0.0f}, {}}};
-            s.first = k == 0;
-            s.x = k & 1;
-            if (k == 0) sym<1, ONES, ONES, true>(s);
-            else sym<1, HI_PAIRS, ONES, true>(s);
-            s = SymLaunch{{{0, 0, 1, 0, (float)(c[2] * pow2(eb - 2 * ea)), (float)(c[1] * pow2(eb - ea)), 0.0f}, {}}};
-            sym<1, ONES, ONES, false>(s);
-            apply<true>(Apply{1, k & 1, k == 0, pow2(ex2 - eb - ex), (float)(c[0] * pow2(ex2 - ex)), eps}, last);
-            lambda = b.lambda;
-            ex = ex2;
-        }
-        return err;
+        if (ap.first) last ? apply<FIRST, true>(ap) : apply<FIRST, false>(ap);
+        else last ? apply<PAIRS, true>(ap) : apply<PAIRS, false>(ap);
     }
 
     hipError_t go(int steps, const double* coef) {
         if (!std::is_same<T, f16>::value) run(k_orth_amax<T>, number(tb, amax_wgs), 0);
         run(k_orth_prep<T>, number(tb, prep_wgs), 0);
-        if constexpr (std::is_same<T, bf16>::value)
-            if (direct(steps)) return go_direct(steps, coef);
         double lambda = 1.0;
         int xt = 0, ex = 0, step = 0;  // X is stored times 2^ex (and 1 / norm_factor in the first block)
         for (bool first = true; step < steps; first = false) {
@@ -1145,8 +1073,8 @@ struct Runner {
             gram.leave = single;
             gram.x = xt;
             Steps list{};
-            if (first) sym<NP, NP, PAIRS, true>(gram);
-            else sym<2, PAIRS, PAIRS, true>(gram);
+            if (first) sym<FIRST, true>(gram);
+            else sym<PAIRS, true>(gram);
             int Q = -1, eq = 0;  // Q: which of the workspace's matrices 2, 3, 4
             double qb = 1.0;
             for (int k = 0; k < len; ++k, ++step) {
@@ -1188,7 +1116,7 @@ struct Runner {
                 run<512>(k_orth_steps, number(tb, [](const OMat&) { return 1; }), STEPS_LDS, list);
             }
             const int ex2 = exponent(sqrt(lambda));
-            apply<false>(Apply{Q, xt, first, pow2((last ? 0 : ex2) - eq - ex), 0.0f, eps}, last);
+            apply(Apply{Q, xt, first, pow2((last ? 0 : ex2) - eq - ex), eps}, last);
             xt ^= 1;
             ex = ex2;
         }
