@@ -1,6 +1,6 @@
 """GPU parity of the Newton-Schulz orthogonalisation where its rounding counts
 most: flat, Gaussian, trained-like and steeply falling spectra, one to eight active
-rows of equal norm, and coefficients with steep slopes, against the iteration in
+rows of equal norm or directions of equal weight, and coefficients with steep slopes, against the iteration in
 64 bits on the CPU.
 
 Tolerance (2-norms over that of the result).  The result's own rounding to its type
@@ -86,11 +86,12 @@ def spectra(m, n, gen):
         rows = torch.randn(k, n, generator=gen)
         g[torch.randperm(m, generator=gen)[:k]] = rows / rows.norm(dim=1, keepdim=True)
         yield f"{k} rows", g
+        yield f"{k} directions", u[:, :k] @ v[:, :k].t()
 
 
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("coef", [ABC, STEEP, ABC[:3]], ids=["default", "steep", "three"])
-@pytest.mark.parametrize("m,n", [(64, 576), (256, 256), (200, 700)])
+@pytest.mark.parametrize("m,n", [(64, 576), (100, 90), (256, 256), (200, 700), (1030, 515), (1200, 1300)])
 def test_spectra(m, n, coef, dtype):
     log(f"[orthogonalize] spectra of {m} x {n} {dtype}, {len(coef)} steps")
     for name, g in spectra(m, n, torch.Generator().manual_seed(m + n)):
@@ -101,3 +102,22 @@ def test_spectra(m, n, coef, dtype):
         allowed = (exact.to(DT[dtype]).double() - exact).norm().item() / size + off_before_rounding(g, coef)
         off = (got - exact).norm().item() / size
         assert off <= allowed, f"{name}: {off:.2e} off, {allowed:.2e} allowed"
+
+
+@pytest.mark.parametrize("m,n", [(64, 576), (512, 1024), (300, 900)])
+def test_bf16_results_are_the_exact_ones_rounded(m, n):
+    """An iteration in 32 bits is off by d, and four times that where matrices have two bits fewer.  A value
+    whose rounding that changes lies within d of a border of its step of 2 h, in d / h of all places: at most the
+    mean of that share differs from the exact result rounded (twice what errors of either sign give)."""
+    log(f"[orthogonalize] rounded results of {m} x {n}")
+    for name, g in spectra(m, n, torch.Generator().manual_seed(7 * m + n)):
+        if name[0].isdigit():  # (of few directions: their errors are no sample)
+            continue
+        g = g.bfloat16()
+        exact = iteration(g, ABC)
+        d = 4 * (iteration(g, ABC, torch.float32).double() - exact).norm().item() / exact.numel() ** 0.5
+        half = torch.ldexp(torch.ones_like(exact), torch.frexp(exact)[1] - 9)  # (frexp: [0.5, 1), steps of 2^-8 of 1)
+        share = (d / half).clamp_max(1.0).mean().item()
+        got = sb.orthogonalize(g.cuda(), eps=EPS).cpu()
+        differ = (got != exact.bfloat16()).double().mean().item()
+        assert differ <= share, f"{name}: {differ:.2e} of the values differ, {share:.2e} allowed"
