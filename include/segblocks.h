@@ -558,7 +558,9 @@ int segblocks_log_probs_backward(const void* logits, int dtype, int layout, int 
 /* One update of segblocks_orthogonalize: `batch` matrices of rows x cols in
  * row-major memory (a filter [C_out,C_in,K,K] is C_out rows of C_in*K*K in
  * either layout), `ld` elements between rows and `batch_stride` between
- * matrices.  Device pointers. */
+ * matrices.  Results do not overlap: they lie matrix after matrix, or rows of
+ * all matrices in turn (batch_stride_out >= cols, ld_out past the last one's
+ * columns).  Device pointers. */
 typedef struct {
     const void* update;
     void* out;

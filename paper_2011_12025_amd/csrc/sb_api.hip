@@ -1193,10 +1193,14 @@ int check_matrices(const char* fn, const sb_matrix* mats, int count, int dtype, 
         if (q.ld < q.cols || q.ld_out < q.cols)
             return fail(SB_EINVAL, fn, "rows of entry %d overlap (ld %lld, ld_out %lld for %d columns)", i, q.ld, q.ld_out,
                         q.cols);
-        const long long one = (q.rows - 1) * q.ld_out + q.cols;
         if (q.ld > (1LL << 36) || q.ld_out > (1LL << 36) || q.batch_stride < 0 || q.batch_stride > (1LL << 44) ||
-            q.batch_stride_out > (1LL << 44) || (q.batch > 1 && q.batch_stride_out < one))
+            (q.batch > 1 && (q.batch_stride_out < 0 || q.batch_stride_out > (1LL << 44))))
             return fail(SB_EINVAL, fn, "bad strides of entry %d", i);
+        // results matrix after matrix, or rows of all matrices in turn
+        const bool after = q.batch_stride_out >= (q.rows - 1) * q.ld_out + q.cols;
+        const bool in_turn = q.batch_stride_out >= q.cols && (q.ld_out - q.cols) / q.batch_stride_out >= q.batch - 1;
+        if (q.batch > 1 && !after && !in_turn)
+            return fail(SB_EINVAL, fn, "bad strides of entry %d: its results overlap", i);
         v.push_back({q.update, q.out, q.ld, q.ld_out, q.batch > 1 ? q.batch_stride : 0,
                      q.batch > 1 ? q.batch_stride_out : 0, q.batch, q.rows, q.cols});
     }
