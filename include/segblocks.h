@@ -560,7 +560,9 @@ int segblocks_log_probs_backward(const void* logits, int dtype, int layout, int 
  * either layout), `ld` elements between rows and `batch_stride` between
  * matrices.  Results do not overlap: they lie matrix after matrix, or rows of
  * all matrices in turn (batch_stride_out >= cols, ld_out past the last one's
- * columns).  Device pointers. */
+ * columns).  No result overlaps an update, another result or the workspace, but
+ * entries with rows at one distance may be different columns of one buffer.
+ * Device pointers. */
 typedef struct {
     const void* update;
     void* out;

@@ -115,6 +115,51 @@ bool any_overlap(const std::vector<Range>& outs, const std::vector<Range>& ins) 
     return false;
 }
 
+// Memory of an update: within `bytes` from p, in runs of `width` bytes at multiples
+// of `pitch` (width = bytes: one run).
+struct Runs : Range {
+    long long pitch, width;
+};
+
+Runs runs_of(const void* p, int batch, int m, int n, long long ld, long long stride, long long es) {
+    const long long bytes = ((batch - 1) * stride + (m - 1) * ld + n) * es;
+    if (m == 1) ld = stride;  // (single rows: those of the matrices)
+    if (ld >= n && stride % ld == 0) return Runs{{p, bytes}, ld * es, n * es};
+    const long long all = (batch - 1) * stride + n;  // the rows of all matrices in turn
+    return all <= ld ? Runs{{p, bytes}, ld * es, all * es} : Runs{{p, bytes}, bytes, bytes};
+}
+
+// Whether two share a byte; those of one pitch may be columns of one buffer.
+bool overlap(const Runs& a, const Runs& b) {
+    if (!overlap((const Range&)a, (const Range&)b)) return false;
+    const bool one_a = a.width == a.bytes, one_b = b.width == b.bytes;
+    if ((one_a && one_b) || (!one_a && !one_b && a.pitch != b.pitch)) return true;
+    const long long pitch = one_a ? b.pitch : a.pitch;
+    const long long apart = (const char*)b.p - (const char*)a.p, d = (apart % pitch + pitch) % pitch;
+    return d < a.width || d + b.width > pitch;
+}
+
+// any_overlap for long lists: where ranges do not reach into each other, each is
+// looked at with its neighbours alone.
+bool list_overlap(std::vector<Runs> outs, const std::vector<Runs>& ins) {
+    auto end = [](const Range& r) { return (const char*)r.p + r.bytes; };
+    std::sort(outs.begin(), outs.end(),
+              [](const Runs& a, const Runs& b) { return std::less<const void*>()(a.p, b.p); });
+    std::vector<const char*> reach;  // the furthest end of an output and those before it
+    for (size_t i = 0; i < outs.size(); ++i) {
+        reach.push_back(i ? std::max(reach[i - 1], end(outs[i])) : end(outs[i]));
+        for (size_t j = i + 1; j < outs.size() && (const char*)outs[j].p < end(outs[i]); ++j)
+            if (overlap(outs[i], outs[j])) return true;
+    }
+    for (const Runs& r : ins) {
+        size_t i = std::lower_bound(outs.begin(), outs.end(), end(r),
+                                    [](const Runs& o, const char* e) { return (const char*)o.p < e; }) - outs.begin();
+        for (; i > 0 && reach[i - 1] > (const char*)r.p; --i)
+            if (overlap(outs[i - 1], r)) return true;
+    }
+    return false;
+}
+
 }  // namespace
 
 extern "C" {
@@ -1207,19 +1252,6 @@ int check_matrices(const char* fn, const sb_matrix* mats, int count, int dtype, 
     return SB_OK;
 }
 
-// any_overlap for long lists.
-bool list_overlap(std::vector<Range> outs, const std::vector<Range>& ins) {
-    auto before = [](const Range& a, const Range& b) { return std::less<const void*>()(a.p, b.p); };
-    std::sort(outs.begin(), outs.end(), before);
-    for (size_t i = 1; i < outs.size(); ++i)
-        if (overlap(outs[i - 1], outs[i])) return true;
-    for (const Range& r : ins) {
-        const auto at = std::upper_bound(outs.begin(), outs.end(), r, before);
-        if ((at != outs.end() && overlap(*at, r)) || (at != outs.begin() && overlap(*(at - 1), r))) return true;
-    }
-    return false;
-}
-
 }  // namespace
 
 int segblocks_orthogonalize(const sb_matrix* matrices, int count, int dtype, int steps, const double* coefficients,
@@ -1234,16 +1266,16 @@ int segblocks_orthogonalize(const sb_matrix* matrices, int count, int dtype, int
         if (!(fabs(coefficients[i]) <= 1e4)) return fail(SB_EINVAL, fn, "coefficient %d is not in [-1e4, 1e4]", i);
     if (!(eps >= 0.0) || !(eps <= 1e30)) return fail(SB_EINVAL, fn, "eps must be in [0, 1e30]");
     const long long es = esize(dtype);
-    std::vector<Range> ins, outs;
+    std::vector<Runs> ins, outs;
     for (int i = 0; i < count; ++i) {
         const sb::OrthMat& q = v[(size_t)i];
         if (!q.g || !q.o) return fail(SB_EINVAL, fn, "update or out of entry %d is NULL", i);
-        ins.push_back({q.g, ((q.batch - 1) * q.bstride + (q.m - 1) * q.ld + q.n) * es});
-        outs.push_back({q.o, ((q.batch - 1) * q.bstride_o + (q.m - 1) * q.ld_o + q.n) * es});
+        ins.push_back(runs_of(q.g, q.batch, q.m, q.n, q.ld, q.bstride, es));
+        outs.push_back(runs_of(q.o, q.batch, q.m, q.n, q.ld_o, q.bstride_o, es));
     }
     const size_t need = sb::orth_ws_bytes(dtype, v.data(), count);
     if ((s = check_ws(fn, need, workspace, ws_bytes))) return s;
-    outs.push_back({workspace, (long long)need});
+    outs.push_back(Runs{{workspace, (long long)need}, (long long)need, (long long)need});
     if (list_overlap(outs, ins)) return fail(SB_EINVAL, fn, "outputs or the workspace overlap inputs or each other");
     return hip_status(fn, sb::launch_orth(dtype, v.data(), count, steps, coefficients, eps, sb::Ws{workspace, need},
                                           stream));

@@ -81,3 +81,64 @@ def test_results_of_a_batch_may_interleave_but_not_overlap(kw, code):
     assert b.lib().segblocks_orthogonalize_workspace_size(ctypes.pointer(entry(**kw)), 1, 0, ctypes.byref(n)) == code
     if code:
         assert "strides" in b.lib().segblocks_last_error().decode()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_updates_and_results_in_columns_of_one_buffer(_gpu, dtype):
+    log(f"[orthogonalize] columns of one buffer {dtype}")
+    gen = torch.Generator().manual_seed(11)
+    cols = [40, 24, 1, 130, 8]
+    buf = torch.randn(70, 2 * sum(cols) + 6, generator=gen).to(DT[dtype]).cuda()
+    before, at, updates, outs = buf.clone(), 3, [], []
+    for n in cols:  # an update, its result, the next update
+        updates.append(buf[:, at:at + n])
+        outs.append(buf[:, at + n:at + 2 * n])
+        at += 2 * n
+    sb.orthogonalize(updates, out=outs)
+    for g, o in zip(updates, outs):
+        near_exact(o[None], g[None], f"{g.shape[1]} columns")
+    for o in outs:
+        o.copy_(before[:, o.storage_offset():o.storage_offset() + o.shape[1]])
+    assert torch.equal(buf, before)
+    # a batch in the rows of one buffer with another one's columns, and single rows between them
+    many = torch.zeros(4, 30, 50, dtype=DT[dtype], device="cuda")
+    rows = many.view(120, 50)
+    batch = torch.randn(4, 30, 20, generator=gen).to(DT[dtype]).cuda()
+    row = torch.randn(1, 10, generator=gen).to(DT[dtype]).cuda()
+    whole = torch.randn(120, 15, generator=gen).to(DT[dtype]).cuda()
+    sb.orthogonalize([batch, row, whole], out=[many[:, :, :20], rows[7:8, 20:30], rows[:, 30:45]])
+    near_exact(many[:, :, :20], batch, "a batch")
+    near_exact(rows[7:8, 20:30][None], row[None], "a row")
+    near_exact(rows[:, 30:45][None], whole[None], "all rows")
+    assert int((many != 0).sum()) <= 120 * 35 + 10
+
+
+def at_bytes(offset):
+    return 0x100000000 + 2 * offset  # (fp16; never read or written)
+
+
+@pytest.mark.parametrize("entries", [
+    # (update, out, rows, cols, ld_out, batch, batch_stride_out) in elements from one place
+    [(1 << 20, 0, 8, 10, 64, 1, 0), (1 << 21, 9, 8, 10, 64, 1, 0)],           # columns that share one
+    [(1 << 20, 0, 8, 10, 64, 1, 0), (1 << 21, 60, 8, 5, 64, 1, 0)],           # columns past the end of a row
+    [(1 << 20, 0, 8, 10, 64, 1, 0), (1 << 21, 128 + 9, 8, 10, 64, 1, 0)],     # two rows on
+    [(1 << 20, 0, 8, 10, 64, 1, 0), (1 << 21, 20, 8, 10, 63, 1, 0)],          # rows at other distances
+    [(1 << 20, 0, 8, 10, 64, 1, 0), (1 << 21, 20, 1, 45, 45, 1, 0)],          # a row that reaches into the next
+    [(1 << 20, 0, 8, 10, 64, 1, 0), (15, 1 << 21, 8, 50, 64, 1, 0)],          # an update on a result
+    [(1 << 20, 0, 8, 10, 64, 2, 16), (1 << 21, 20, 8, 10, 64, 1, 0)],         # rows of a batch in turn
+    [(1 << 20, 0, 8, 10, 64, 2, 640), (1 << 21, 9 + 704, 8, 10, 64, 1, 0)],   # matrix after matrix
+    [(1 << 20, 0, 8, 10, 64, 1, 0), (1 << 21, 20, 8, 10, 64, 1, 0), (1 << 22, 512 - 40, 2, 8, 8, 1, 0)],  # a third one
+])
+def test_results_that_overlap_in_one_buffer_are_refused(entries):
+    for order in (entries, entries[::-1]):
+        mats = (b.Matrix * len(order))()
+        for q, (u, o, m, n, ld, batch, stride) in zip(mats, order):
+            q.batch, q.rows, q.cols, q.ld, q.ld_out = batch, m, n, 64 if n <= 64 else n, ld
+            q.batch_stride, q.batch_stride_out = 1 << 14, stride
+            q.update, q.out = at_bytes(u), at_bytes(o)
+        c = (ctypes.c_double * 3)(1.0, 0.0, 0.0)
+        n = ctypes.c_size_t(0)
+        assert b.lib().segblocks_orthogonalize_workspace_size(mats, len(order), 1, ctypes.byref(n)) == 0
+        code = b.lib().segblocks_orthogonalize(mats, len(order), 1, 1, c, 0.0, ctypes.c_void_p(0x900000000), n.value, None)
+        assert code == -1 and "overlap" in b.lib().segblocks_last_error().decode()
