@@ -1238,8 +1238,9 @@ int check_matrices(const char* fn, const sb_matrix* mats, int count, int dtype, 
         if (q.ld < q.cols || q.ld_out < q.cols)
             return fail(SB_EINVAL, fn, "rows of entry %d overlap (ld %lld, ld_out %lld for %d columns)", i, q.ld, q.ld_out,
                         q.cols);
-        if (q.ld > (1LL << 36) || q.ld_out > (1LL << 36) || q.batch_stride < 0 || q.batch_stride > (1LL << 44) ||
-            (q.batch > 1 && (q.batch_stride_out < 0 || q.batch_stride_out > (1LL << 44))))
+        const long long far = (1LL << 44) / std::max(1, q.batch - 1);  // (a batch's extent stays within 64 bits)
+        if (q.ld > (1LL << 36) || q.ld_out > (1LL << 36) || q.batch_stride < 0 || q.batch_stride > far ||
+            (q.batch > 1 && (q.batch_stride_out < 0 || q.batch_stride_out > far)))
             return fail(SB_EINVAL, fn, "bad strides of entry %d", i);
         // results matrix after matrix, or rows of all matrices in turn
         const bool after = q.batch_stride_out >= (q.rows - 1) * q.ld_out + q.cols;

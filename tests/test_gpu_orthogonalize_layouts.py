@@ -75,6 +75,11 @@ def entry(**kw):
     (dict(ld_out=30, batch_stride_out=40), -1), (dict(ld_out=30, batch_stride_out=-10), -1),
     (dict(rows=1, ld_out=10, batch_stride_out=10), 0), (dict(rows=1, batch_stride_out=9), -1),
     (dict(ld=30, batch_stride=10), 0), (dict(batch_stride=0), 0),
+    # extents past 64 bits, which would wrap to a few elements
+    (dict(rows=1, cols=1, ld=1, ld_out=1, batch=(1 << 20) + 1, batch_stride=1 << 44, batch_stride_out=1), -1),
+    (dict(rows=1, cols=1, ld=1, ld_out=1, batch=(1 << 20) + 1, batch_stride=1, batch_stride_out=1 << 44), -1),
+    (dict(rows=1, cols=1, ld=1, ld_out=1, batch=(1 << 20) + 1, batch_stride=1 << 24, batch_stride_out=1 << 24), 0),
+    (dict(batch=2, batch_stride=1 << 44, batch_stride_out=1 << 44), 0),
 ])
 def test_results_of_a_batch_may_interleave_but_not_overlap(kw, code):
     n = ctypes.c_size_t(0)
