@@ -583,7 +583,10 @@ typedef struct {
  * The sums are fp32, and matrices between the products are held to 22 bits
  * and a sign, for 16-bit updates too, whose result is rounded once.  Workspace:
  * segblocks_orthogonalize_workspace_size (a function of the entries' sizes,
- * pointers not looked at). */
+ * pointers not looked at): about 12 bytes an element and 20 for each of the
+ * shorter side squared, for as many matrices as fill the chip (2^34 elements
+ * of 32768 rows take 228 GB beside the update and its result, which with 288 GB
+ * of memory leaves room for 16-bit ones alone). */
 int segblocks_orthogonalize(const sb_matrix* matrices, int count, int dtype, int steps, const double* coefficients,
                             double eps, void* workspace, size_t ws_bytes, hipStream_t stream);
 int segblocks_orthogonalize_workspace_size(const sb_matrix* matrices, int count, int dtype, size_t* bytes);

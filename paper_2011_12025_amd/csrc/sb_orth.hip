@@ -73,11 +73,11 @@ constexpr int MAXP = 1024;  // workgroups that make X, each with its sum of squa
 constexpr int MAXA = 1024;  // workgroups that look for the largest value
 constexpr long long W_SUM = 4 * MAXA, W_X = W_SUM + 4 * MAXP;  // [0]: the largest values
 __host__ __device__ inline long long w_x_bytes(int sp, int Lp) { return (long long)sp * Lp * 4; }
-// X and its transpose, each twice: a block's and the next one's
-__host__ __device__ inline long long w_x(int sp, int Lp, int i) { return W_X + i * w_x_bytes(sp, Lp); }
-__host__ __device__ inline long long w_xt(int sp, int Lp, int i) { return W_X + (2 + i) * w_x_bytes(sp, Lp); }
+// X, of which a block needs no more than X X^T, and its transpose twice: a block's
+// and the next one's
+__host__ __device__ inline long long w_xt(int sp, int Lp, int i) { return W_X + (1 + i) * w_x_bytes(sp, Lp); }
 __host__ __device__ inline long long w_sym(int sp, int Lp, int i) {
-    return W_X + 4 * w_x_bytes(sp, Lp) + i * ((long long)sp * sp * 4);
+    return W_X + 3 * w_x_bytes(sp, Lp) + i * ((long long)sp * sp * 4);
 }
 constexpr int SYMS = 5;  // A, T and three that P and Q take in turn
 
@@ -247,7 +247,7 @@ __global__ __launch_bounds__(WG) void k_orth_prep(Table tb) {
     const int e = scale_of(q, ws), tid = (int)threadIdx.x;
     const bool tall = q.m > q.n;
     const int mp = tall ? q.Lp : q.sp, np = tall ? q.sp : q.Lp, tn = np / 64, tiles = (mp / 64) * tn, wgs = prep_wgs(q);
-    char* X = ws + w_x(q.sp, q.Lp, 0);      // [sp][Lp]
+    char* X = ws + W_X;                     // [sp][Lp]
     char* Xt = ws + w_xt(q.sp, q.Lp, 0);    // [Lp][sp]
     float sum = 0.0f;
     for (int t = p.t; t < tiles; t += wgs) {
@@ -533,7 +533,6 @@ struct SymLaunch {
     SymJob job[2];
     int tiles;  // of one product
     int whole, parts, first;
-    int x;      // of X X^T: which X
     int leave;  // sums of every tile, for k_orth_steps
     float eps;
     float* sums;  // [unit][T * T], units counted from the first split tile's (whole < 0: from the first of all)
@@ -586,7 +585,7 @@ __global__ __launch_bounds__(NT<T>, 2) void k_orth_sym(Table tb, SymLaunch s) {
     const int K = GRAM ? q.Lp : q.sp, steps = K / STEP_K<T, S, S>;
     const int k0 = (int)((long long)steps * u.part / u.parts), k1 = (int)((long long)steps * (u.part + 1) / u.parts);
     const long long pitch = (long long)K * (2 * S);
-    const char* A = GRAM ? ws + w_x(q.sp, q.Lp, s.x) : ws + w_sym(q.sp, q.Lp, j.a);
+    const char* A = GRAM ? ws + W_X : ws + w_sym(q.sp, q.Lp, j.a);
     const char* B = GRAM ? A : ws + w_sym(q.sp, q.Lp, j.b);
     product_tile<T, S, S>(A + bi * T * pitch, pitch, B + bj * T * pitch, pitch, k0, k1 - k0, lds);
     float* C = (float*)lds;
@@ -816,7 +815,7 @@ __global__ __launch_bounds__(NT<T>, 2) void k_orth_apply(Table tb, Apply ap) {
                     if (c + n < q.n) to[n] = v.e[n];
         }
     } else {
-        store_tile<T, PAIRS, false>(C, ws + w_x(q.sp, q.Lp, ap.xt ^ 1), q.Lp, i * T, k * T);
+        store_tile<T, PAIRS, false>(C, ws + W_X, q.Lp, i * T, k * T);
         store_tile<T, PAIRS, true>(C, ws + w_xt(q.sp, q.Lp, ap.xt ^ 1), q.sp, k * T, i * T);
     }
 }
@@ -917,11 +916,12 @@ std::vector<Group> groups_of(const OrthMat* mats, int count) {
             o.ws_one = up(w_sym(o.sp, o.Lp, SYMS), 256);
             g.bytes += (size_t)(o.ws_one * o.batch);
         }
-        // sums of X X^T and, where a product has a remainder to split, of that
+        // sums of X X^T where it is split (or left for k_orth_steps) and, where a product
+        // has a remainder to split, of that
         g.sums = g.bytes;
         const long long n128 = unit == 128 ? sym_count(g.tb, 128) : 0, n64 = sym_count(g.tb, 64);
         const int T = tile_of(n128, unit == 128);
-        long long cells = gram_units(g.tb, T) * T * T;
+        long long cells = unit == 64 || (T == 128 ? n128 : n64) < SLOTS ? gram_units(g.tb, T) * T * T : 0;
         for (int jobs = 1; jobs <= 2; ++jobs) {
             const int t = tile_of(n128 * jobs, unit == 128);
             if ((t == 128 ? n128 : n64) * jobs >= SLOTS) cells = std::max(cells, (long long)SLOTS * t * t);
@@ -1075,7 +1075,6 @@ struct Runner {
             SymLaunch gram{{{0, 0, 0, -1, pow2(ea - 2 * ex), 0.0f, 0.0f}, {}}};
             gram.first = first;
             gram.leave = single;
-            gram.x = xt;
             Steps list{};
             if (first) sym<FIRST, true>(gram);
             else sym<PAIRS, true>(gram);

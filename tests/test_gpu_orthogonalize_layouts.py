@@ -147,3 +147,14 @@ def test_results_that_overlap_in_one_buffer_are_refused(entries):
         assert b.lib().segblocks_orthogonalize_workspace_size(mats, len(order), 1, ctypes.byref(n)) == 0
         code = b.lib().segblocks_orthogonalize(mats, len(order), 1, 1, c, 0.0, ctypes.c_void_p(0x900000000), n.value, None)
         assert code == -1 and "overlap" in b.lib().segblocks_last_error().decode()
+
+
+@pytest.mark.parametrize("m,n", [(64, 1 << 20), (4096, 4096), (4096, 16384), (32768, 1 << 18)])
+def test_workspace_takes_twelve_bytes_an_element(m, n):
+    """X and two transposes in pairs, five matrices of the shorter side, sums of tiles (up to 128 KB a CU) and 8 KB."""
+    size = ctypes.c_size_t(0)
+    for dtype in (0, 1, 2):
+        for rows, cols in ((m, n), (n, m)):
+            q = b.Matrix(batch=1, rows=rows, cols=cols, ld=cols, ld_out=cols)
+            assert b.lib().segblocks_orthogonalize_workspace_size(ctypes.pointer(q), 1, dtype, ctypes.byref(size)) == 0
+            assert size.value <= 12 * m * n + 20 * m * m + 512 * 65536 + 8192 + 256
