@@ -581,7 +581,10 @@ typedef struct {
  * zeros, one with NaN or an infinity gives NaN.  A matrix has up to 2^34
  * elements, a longer side of up to 2^23 and a shorter one of up to 32768.
  * The sums are fp32, and matrices between the products are held to 22 bits
- * and a sign, for 16-bit updates too, whose result is rounded once.  Workspace:
+ * and a sign, for 16-bit updates too, whose result is rounded once.  The same
+ * call gives the same bits; the sizes of the other entries (not their values)
+ * decide how its sums are split, so an update has other last bits, of the same
+ * precision, among others than alone.  Workspace:
  * segblocks_orthogonalize_workspace_size (a function of the entries' sizes,
  * pointers not looked at): about 12 bytes an element and 20 for each of the
  * shorter side squared, for as many matrices as fill the chip (2^34 elements

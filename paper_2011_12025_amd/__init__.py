@@ -912,10 +912,11 @@ def orthogonalize(updates, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315
 
     ``updates``: a matrix [m, n], a batch of them [B, m, n] or a filter [C_out,
     C_in, K, K] (taken as [C_out, C_in K K]), or a list of such tensors of one
-    type and device, which go through the same launches.  ``coefficients``: (a, b,
-    c), or one such triple for every step.  Returns tensors shaped and ordered
-    like the updates (``out`` if given).  ``workspace`` as in block_conv3x3, sized
-    by orthogonalize_workspace_size()."""
+    type and device, which go through the same launches (their sizes decide how sums
+    are split: an update's last bits differ among others and alone, its precision
+    does not).  ``coefficients``: (a, b, c), or one such triple for every step.
+    Returns tensors shaped and ordered like the updates (``out`` if given).
+    ``workspace`` as in block_conv3x3, sized by orthogonalize_workspace_size()."""
     single = isinstance(updates, torch.Tensor)
     updates = [updates] if single else list(updates)
     if not updates:

@@ -121,3 +121,28 @@ def test_bf16_results_are_the_exact_ones_rounded(m, n):
         got = sb.orthogonalize(g.cuda(), eps=EPS).cpu()
         differ = (got != exact.bfloat16()).double().mean().item()
         assert differ <= share, f"{name}: {differ:.2e} of the values differ, {share:.2e} allowed"
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_an_update_among_others(dtype):
+    """The same update alone and beside smaller, larger, longer and many others: within the same tolerance
+    (sums are split by the sizes of the call), and the others' values have no part in it."""
+    log(f"[orthogonalize] one update in lists {dtype}")
+    gen = torch.Generator().manual_seed(21)
+    def random(m, n):
+        return torch.randn(m, n, generator=gen).to(DT[dtype]).cuda()
+    for m, n in [(64, 576), (40, 50), (200, 190), (512, 512)]:
+        for name, g in spectra(m, n, gen):
+            if name not in ("gaussian", "falling", "1 directions", "4 rows"):
+                continue
+            g = g.to(DT[dtype])
+            exact = iteration(g, ABC)
+            size = exact.norm().item()
+            allowed = (exact.to(DT[dtype]).double() - exact).norm().item() / size + off_before_rounding(g, ABC)
+            g = g.cuda()
+            for others in ([], [(8, 20)], [(900, 900)], [(64, 9000)], [(1500, 1500), (70, 4000)], [(30, 40)] * 40):
+                mats = [random(*s) for s in others]
+                got = sb.orthogonalize([g] + mats, eps=EPS)[0]
+                off = (got.double().cpu() - exact).norm().item() / size
+                assert off <= allowed, f"{m} x {n} {name} beside {others}: {off:.2e} off, {allowed:.2e} allowed"
+                assert torch.equal(got, sb.orthogonalize([g] + [2 * t + 1 for t in mats], eps=EPS)[0])
