@@ -1135,7 +1135,7 @@ long long scores_bytes(long long R, long long P, int C, int C_buf, int es) {
 
 int segblocks_log_probs(const void* logits, int dtype, int layout, int N, int C, int H, int W, int C_buf,
                         const int64_t* labels, long long ignore, int topk, float* logp, float* lse, float* entropy,
-                        float* top_logp, int32_t* top_index, void* workspace, size_t ws_bytes, hipStream_t stream) {
+                        float* top_logp, int32_t* top_index, void* workspace, size_t ws_bytes, hipStream_t stream) try {
     const char* fn = "segblocks_log_probs";
     sb::LogpArgs a{};
     int s;
@@ -1164,10 +1164,13 @@ int segblocks_log_probs(const void* logits, int dtype, int layout, int N, int C,
     if (need && any_overlap({{workspace, (long long)need}}, {rz, rl, outs[0], outs[1], outs[2], outs[3], outs[4]}))
         return fail(SB_EINVAL, fn, "the workspace overlaps an argument");
     return hip_status(fn, sb::launch_logp(dtype, a, sb::Ws{workspace, need}, stream));
+} catch (const std::bad_alloc&) {  // (the lists above and messages, on the host)
+    g_err.clear();
+    return SB_ENOMEM;
 }
 
 int segblocks_log_probs_workspace_size(int dtype, int layout, int N, int C, int H, int W, int C_buf, int topk,
-                                       size_t* bytes) {
+                                       size_t* bytes) try {
     const char* fn = "segblocks_log_probs_workspace_size";
     sb::LogpArgs a{};
     int s;
@@ -1179,12 +1182,15 @@ int segblocks_log_probs_workspace_size(int dtype, int layout, int N, int C, int 
     *bytes = sb::logp_ws_bytes(dtype, a);
     g_err.clear();
     return SB_OK;
+} catch (const std::bad_alloc&) {
+    g_err.clear();
+    return SB_ENOMEM;
 }
 
 int segblocks_log_probs_backward(const void* logits, int dtype, int layout, int N, int C, int H, int W, int C_buf,
                                  const int64_t* labels, long long ignore, const float* lse, const float* d_logp,
                                  const float* entropy, const float* d_entropy, int topk, const int32_t* top_index,
-                                 const float* d_top, int C_dbuf, void* dlogits, hipStream_t stream) {
+                                 const float* d_top, int C_dbuf, void* dlogits, hipStream_t stream) try {
     const char* fn = "segblocks_log_probs_backward";
     sb::LogpGradArgs a{};
     int s;
@@ -1218,6 +1224,9 @@ int segblocks_log_probs_backward(const void* logits, int dtype, int layout, int 
                      {entropy, f}, {d_entropy, f}, {top_index, f * topk}, {d_top, f * topk}}))
         return fail(SB_EINVAL, fn, "dlogits overlaps an input");
     return hip_status(fn, sb::launch_logp_grad(dtype, a, stream));
+} catch (const std::bad_alloc&) {
+    g_err.clear();
+    return SB_ENOMEM;
 }
 
 namespace {
@@ -1280,7 +1289,7 @@ int segblocks_orthogonalize(const sb_matrix* matrices, int count, int dtype, int
     if (list_overlap(outs, ins)) return fail(SB_EINVAL, fn, "outputs or the workspace overlap inputs or each other");
     return hip_status(fn, sb::launch_orth(dtype, v.data(), count, steps, coefficients, eps, sb::Ws{workspace, need},
                                           stream));
-} catch (const std::bad_alloc&) {  // (the lists above, on the host)
+} catch (const std::bad_alloc&) {
     g_err.clear();
     return SB_ENOMEM;
 }
