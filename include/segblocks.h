@@ -549,7 +549,7 @@ int segblocks_log_probs_workspace_size(int dtype, int layout, int N, int C, int 
  * -inf has the gradient 0; a label or top_index outside [0, C) (and not
  * `ignore`) makes its row NaN.  dlogits is laid out like logits with C_dbuf
  * channels, of which the first C are written and the others left as they
- * are. */
+ * are (logits may be among them: different channels of one buffer). */
 int segblocks_log_probs_backward(const void* logits, int dtype, int layout, int N, int C, int H, int W, int C_buf,
                                  const int64_t* labels, long long ignore, const float* lse, const float* d_logp,
                                  const float* entropy, const float* d_entropy, int topk, const int32_t* top_index,

@@ -797,7 +797,8 @@ def log_probs_backward(logits: torch.Tensor, labels, lse: torch.Tensor, d_logp=N
     float32, shaped like those results) and the forward call's labels, lse,
     entropy and top_index.  ``out``: a tensor shaped and ordered like ``logits``
     to write to, such as the first channels of the map that a layer's backward
-    pass takes (its other channels are left as they are)."""
+    pass takes (its other channels are left as they are), or channels of the
+    scores' own buffer past the classes."""
     device, dt = _device_of(logits), _dt(logits)
     if device != _current_device():
         with torch.cuda.device(device):

@@ -115,8 +115,8 @@ bool any_overlap(const std::vector<Range>& outs, const std::vector<Range>& ins) 
     return false;
 }
 
-// Memory of an update: within `bytes` from p, in runs of `width` bytes at multiples
-// of `pitch` (width = bytes: one run).
+// Memory within `bytes` from p, in runs of `width` bytes at multiples of `pitch`
+// (width = bytes: one run).
 struct Runs : Range {
     long long pitch, width;
 };
@@ -1219,9 +1219,11 @@ int segblocks_log_probs_backward(const void* logits, int dtype, int layout, int 
     a.topk = topk;
     const long long f = a.R * 4;
     const int es = esize(dtype);
-    if (any_overlap({{dlogits, scores_bytes(a.R, a.P, C, C_dbuf, es)}},
-                    {{logits, scores_bytes(a.R, a.P, C, C_buf, es)}, {labels, a.R * 8}, {lse, f}, {d_logp, f},
-                     {entropy, f}, {d_entropy, f}, {top_index, f * topk}, {d_top, f * topk}}))
+    const Range out{dlogits, scores_bytes(a.R, a.P, C, C_dbuf, es)}, in{logits, scores_bytes(a.R, a.P, C, C_buf, es)};
+    // (the scores and their gradient may be different channels of one buffer)
+    if (overlap(Runs{out, C_dbuf * a.P * es, C * a.P * es}, Runs{in, C_buf * a.P * es, C * a.P * es}) ||
+        any_overlap({out}, {{labels, a.R * 8}, {lse, f}, {d_logp, f}, {entropy, f}, {d_entropy, f}, {top_index, f * topk},
+                            {d_top, f * topk}}))
         return fail(SB_EINVAL, fn, "dlogits overlaps an input");
     return hip_status(fn, sb::launch_logp_grad(dtype, a, stream));
 } catch (const std::bad_alloc&) {
